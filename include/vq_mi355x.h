@@ -381,6 +381,113 @@ size_t vq_attn_decode_workspace(const vq_kv_t *kv);
 int vq_kv_quantize(const vq_kv_t *kv, const void *k_new, const void *v_new, int n_new, int pos, void *stream);
 
 /*
+ * A VQ-compressed KV cache of one layer in PAGES, for requests that come and go and whose lengths differ (continuous
+ * batching): the codes of Sec. III-A as in vq_kv_t, but a request's tokens lie in pages of page_tokens tokens that a block
+ * table names.  One pool per layer; block tables and slots are the same for all layers of a model.
+ *   token t of request b: page = block_table[b][t / page_tokens], offset o = t % page_tokens
+ *   K codes: k_codes[page][h][o][p]
+ *   V codes: v_codes[page][h][o / 16][p][o % 16]    (sub-vector-major in blocks of 16 tokens: the product with V contracts over
+ *            tokens, so a lane of the matrix operand takes eight tokens of one sub-vector, here eight consecutive bytes)
+ * Codebooks, p, v and cb_groups as in vq_kv_t.  H is the number of CACHE heads; query heads are a multiple of it.
+ * A slot is page * page_tokens + offset.
+ */
+typedef struct vq_kv_pages_t {
+    int H, D, v;             /* cache heads, head dim, sub-vector length 2, 4 or 8 */
+    int n_entries;           /* E <= 256 */
+    int cb_groups;           /* G codebooks per (head, side); divides D/v */
+    int n_pages;
+    int page_tokens;         /* 16, 32, 64, 128 or 256; n_pages * page_tokens < 2^31 */
+    const void *k_codes;     /* device, uint8 [n_pages][H][page_tokens][D/v] */
+    const void *v_codes;     /* device, uint8 [n_pages][H][page_tokens/16][D/v][16] */
+    const void *k_codebooks; /* device, fp16 [H][G][E][v] */
+    const void *v_codebooks; /* device, fp16 [H][G][E][v] */
+} vq_kv_pages_t;
+
+/*
+ * The pages of one step, on the GPU: what vq_kv_quantize_paged and vq_attn_paged of every layer of the step read, from the
+ * lengths that the requests have and get.  A request is a row of the block table.
+ *   1. new_lens[b] < 0: the request has ended.  Its ceil(lens[b] / page_tokens) pages go back on the pool, in order of b and
+ *      then of the table; its length becomes 0.
+ *   2. new_lens[b] >= 0: it gets room for that many tokens behind its lens[b].  Pages are taken from the pool's end (free_pages[n_free - 1]
+ *      first), in order of b, and written to the table behind those it has.
+ *   A request is refused (status[b] = 1: no tokens, no pages, length as it was) if its tokens would not fit the table's row,
+ *   if the new tokens of the requests up to it (those that fit their row, refused or not) pass n_tokens, or if it needs pages and
+ *   those needed up to it (by requests not refused for the other reasons) pass the pool.  status[b] is 0 otherwise.
+ * Reads lens, new_lens, n_free, free_pages [0, n_free), block_table; writes everything else below.  With seq_lens and n_free_out apart
+ * from lens and n_free a call may be made again with the same result as long as nobody else changed the arrays; with the same arrays it steps in place.
+ * Table entries behind a request's pages, and free_pages behind the pool's end, are left as they are.
+ * Values that no sequence of such calls produces are bounded, not reported: lens to [0, max_pages * page_tokens], n_free to
+ * [0, n_pages]; a page id outside [0, n_pages) gives slots of -1.  All arrays: device, int32, 4-byte aligned.
+ * No two of them may overlap but for the two pairs above.  Errors: NULL / SHAPE / ALIGN / LAUNCH.
+ */
+typedef struct vq_page_step_t {
+    int B;                 /* requests; 0 <= B <= 65536 */
+    int max_pages;         /* row length of the block table, >= 1; B * max_pages < 2^31 */
+    int page_tokens;       /* as in vq_kv_pages_t */
+    int n_pages;           /* pages of the pool, n_pages * page_tokens < 2^31 */
+    int n_tokens;          /* most new tokens of the step: length of slots and positions, 0 <= n_tokens <= 2^20 */
+    const int *new_lens;   /* [B] */
+    const int *lens;       /* [B] tokens in the cache before the step */
+    int *block_table;      /* [B][max_pages] */
+    int *free_pages;       /* [n_pages] */
+    const int *n_free;     /* [1] */
+    int *seq_lens;         /* [B] tokens in the cache after the step; may be lens */
+    int *n_free_out;       /* [1]; may be n_free */
+    int *cu_new;           /* [B + 1] first new token of every request among the step's, and their number */
+    int *slots;            /* [n_tokens] slot of every new token, -1 behind the last */
+    int *positions;        /* [n_tokens] its position in the request, -1 behind the last; or NULL */
+    int *status;           /* [B] */
+} vq_page_step_t;
+int vq_kv_pages_assign(const vq_page_step_t *step, void *stream);
+
+/*
+ * vq_kv_quantize into pages: the codes of n_tokens new tokens' K and V vectors (the same definition of "closest") are
+ * written to their slots.
+ *   k_new, v_new: device fp16, token i's head h at element i * stride + h * D (k_stride, v_stride >= H * D, multiples of 8, at most
+ *   2^23: the tensors may be parts of a fused projection's output).
+ *   slots: device int32 [n_tokens]; a slot outside [0, n_pages * page_tokens) is skipped (padding).  Slots that are written must differ.
+ *   0 <= n_tokens <= 2^20.
+ * Codebooks of one side of a head must fit 64 KiB, (G * E * v) % 8 == 0 (VQ_ERR_UNSUPPORTED otherwise).
+ */
+int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_stride, const void *v_new, size_t v_stride,
+                         const int *slots, int n_tokens, void *stream);
+
+/*
+ * Attention of the new tokens of a batch of requests over the paged cache, their own codes included: one new token each (a
+ * decode step), a few (drafted tokens), a chunk of a prompt, or any mix.  With pos = seq_lens[b] - n_b + i for new token i of the
+ * n_b = cu_new[b + 1] - cu_new[b] of request b, and h = hq / (Hq / H):
+ *   s(t)    = sm_scale * q[cu_new[b] + i][hq] . K[b][h][t]
+ *   softcap > 0:   s(t) = softcap * tanh(s(t) / softcap)
+ *   slopes:        s(t) = s(t) - slopes[hq] * |pos - t|
+ *   visible(t) = t < seq_lens[b] and ( t <= pos and (window == 0 or t > pos - window)  or  t < prefix_lens[b] )
+ *   out     = softmax over the visible t of s(t) . V[b][h][t]; zeros where nothing is visible
+ * Rows of q and out behind cu_new[B] are neither read nor written.
+ *   q, out: device fp16, token i's head hq at element i * stride + hq * D (strides >= Hq * D, multiples of 8).
+ * Tokens that a row does not attend never matter, with whatever codes behind a request's length; entries that codes of
+ * its tokens point at have to be finite.  Page ids outside [0, n_pages), lengths beyond the table and cu_new beyond n_tokens do not
+ * make the call read or write out of bounds, but leave the request's rows unspecified.
+ * The requests' key ranges are cut into equal shares for the compute units; a share's sums are joined by log-sum-exp in a second
+ * launch, in a fixed order: repeated calls are bit-identical.  ws: vq_attn_paged_workspace(kv, batch) bytes; the query reads only sizes.
+ * D is 64 or 128, D / v / cb_groups a power of two (VQ_ERR_UNSUPPORTED otherwise).
+ */
+typedef struct vq_paged_batch_t {
+    int B;                   /* requests, 0 <= B <= 65536 */
+    int max_pages;           /* row length of the block table, >= 1; B * max_pages < 2^31; max_pages * page_tokens < 2^31 */
+    int n_tokens;            /* rows of q and out: cu_new[B] or more, 0 <= n_tokens <= 2^20 */
+    int Hq;                  /* query heads, a multiple of H */
+    const int *block_table;  /* device, int32 [B][max_pages] */
+    const int *cu_new;       /* device, int32 [B + 1], ascending from 0 */
+    const int *seq_lens;     /* device, int32 [B], tokens in the cache, the new ones among them */
+    const int *prefix_lens;  /* device, int32 [B]: tokens that every new token attends; or NULL (= 0) */
+    const float *slopes;     /* device, fp32 [Hq], or NULL */
+    int window;              /* tokens that a new token looks back on, itself among them; 0: all */
+    float softcap;           /* 0: none */
+} vq_paged_batch_t;
+int vq_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch, const void *q, size_t q_stride, float sm_scale,
+                  void *out, size_t out_stride, void *ws, size_t ws_bytes, void *stream);
+size_t vq_attn_paged_workspace(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch);
+
+/*
  * Test hooks: the dequantized operand itself (Sec. II-A), for bit-exact checks.
  * vq_dequant: W[N][K], fp32 (out_fp32 = 1: the fp32 sum of the residual entries)
  *             or fp16 (out_fp32 = 0: that sum rounded to nearest even).

@@ -53,6 +53,26 @@ class vq_kv_t(ctypes.Structure):
                 ("seq_lens", ctypes.c_void_p)]
 
 
+class vq_kv_pages_t(ctypes.Structure):
+    _fields_ = [("H", ctypes.c_int), ("D", ctypes.c_int), ("v", ctypes.c_int), ("n_entries", ctypes.c_int), ("cb_groups", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_tokens", ctypes.c_int),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_codebooks", ctypes.c_void_p), ("v_codebooks", ctypes.c_void_p)]
+
+
+class vq_page_step_t(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("max_pages", ctypes.c_int), ("page_tokens", ctypes.c_int), ("n_pages", ctypes.c_int), ("n_tokens", ctypes.c_int),
+                ("new_lens", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("n_free", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("n_free_out", ctypes.c_void_p), ("cu_new", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class vq_paged_batch_t(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("max_pages", ctypes.c_int), ("n_tokens", ctypes.c_int), ("Hq", ctypes.c_int),
+                ("block_table", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p),
+                ("slopes", ctypes.c_void_p), ("window", ctypes.c_int), ("softcap", ctypes.c_float)]
+
+
 class vq_gemv_call_t(ctypes.Structure):
     _fields_ = [("w", ctypes.POINTER(ctypes.POINTER(vq_weight_t))), ("x", ctypes.POINTER(ctypes.c_void_p)),
                 ("y", ctypes.POINTER(ctypes.c_void_p)), ("count", ctypes.c_int)]
@@ -109,6 +129,12 @@ SYMBOLS = {
     "vq_kv_dequant": (ctypes.c_int, [ctypes.POINTER(vq_kv_t), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]),
     "vq_kv_quantize": (ctypes.c_int, [ctypes.POINTER(vq_kv_t), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
                                       ctypes.c_int, ctypes.c_void_p]),
+    "vq_kv_pages_assign": (ctypes.c_int, [ctypes.POINTER(vq_page_step_t), ctypes.c_void_p]),
+    "vq_kv_quantize_paged": (ctypes.c_int, [ctypes.POINTER(vq_kv_pages_t), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t,
+                                            ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]),
+    "vq_attn_paged": (ctypes.c_int, [ctypes.POINTER(vq_kv_pages_t), ctypes.POINTER(vq_paged_batch_t), ctypes.c_void_p, ctypes.c_size_t,
+                                     ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "vq_attn_paged_workspace": (ctypes.c_size_t, [ctypes.POINTER(vq_kv_pages_t), ctypes.POINTER(vq_paged_batch_t)]),
     "vq_probe_copy": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "vq_probe_read": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]),
     "vq_probe_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]),
@@ -549,6 +575,140 @@ def vq_kv_dequant(kv: VQKVDev, which: int) -> torch.Tensor:
     out = torch.empty((kv.B, kv.H, kv.T, kv.D), dtype=torch.float16, device=kv.k_codes.device)
     d = kv.desc()
     _check(lib().vq_kv_dequant(ctypes.byref(d), which, _dev(out, "out"), _stream()), "vq_kv_dequant")
+    return out
+
+
+@dataclass
+class VQKVPagesDev:
+    """Device-resident paged VQ KV cache of one layer: uint8 K codes [n_pages][H][page_tokens][D/v], V codes
+    [n_pages][H][page_tokens/16][D/v][16], fp16 codebooks [H][G][E][v]."""
+    H: int
+    D: int
+    v: int
+    page_tokens: int
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_codebooks: torch.Tensor
+    v_codebooks: torch.Tensor
+
+    def desc(self) -> vq_kv_pages_t:
+        _, G, E, _ = self.k_codebooks.shape
+        n_pages = self.k_codes.shape[0]
+        if self.D > 0 and self.v > 0 and self.page_tokens > 0:
+            _want(self.k_codes, "k_codes", (n_pages, self.H, self.page_tokens, self.D // self.v))
+            _want(self.v_codes, "v_codes", (n_pages, self.H, self.page_tokens // 16, self.D // self.v, 16))
+        _want(self.k_codebooks, "k_codebooks", (self.H, G, E, self.v))
+        _want(self.v_codebooks, "v_codebooks", (self.H, G, E, self.v))
+        return vq_kv_pages_t(self.H, self.D, self.v, E, G, n_pages, self.page_tokens,
+                             _here(self.k_codes, "k_codes", torch.uint8), _here(self.v_codes, "v_codes", torch.uint8),
+                             _here(self.k_codebooks, "k_codebooks", torch.float16),
+                             _here(self.v_codebooks, "v_codebooks", torch.float16))
+
+
+def _want(t: torch.Tensor, name: str, shape: tuple) -> None:
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
+
+
+def _here(t: Optional[torch.Tensor], name: str, dtype, shape: Optional[tuple] = None) -> Optional[int]:
+    """``_dev`` for the calls that take several tensors of a step: of this shape, and on the device whose stream the call goes to."""
+    p = _dev(t, name, dtype)
+    if t is not None:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} must be on the current device")
+        if shape is not None:
+            _want(t, name, shape)
+    return p
+
+
+def _rows(t: torch.Tensor, name: str, heads: Optional[int], D: int) -> tuple:
+    """(address, elements between tokens) of fp16 [tokens][heads][D] whose tokens may lie apart (part of a fused projection)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.dtype != torch.float16:
+        raise TypeError(f"{name} must be {torch.float16}, got {t.dtype}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    if t.dim() != 3 or t.shape[2] != D or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must have the shape (tokens, {'heads' if heads is None else heads}, {D}), got {tuple(t.shape)}")
+    row = t.shape[1] * D
+    if t.numel() > 0 and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != D)):
+        raise ValueError(f"{name} must be contiguous within a token")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else row)
+
+
+class VQPagePlan:
+    """What ``vq_kv_pages_assign`` writes for a step of up to ``B`` requests and ``n_tokens`` new tokens: int32 tensors
+    cu_new [B + 1], seq_lens [B], slots [n_tokens], positions [n_tokens], status [B].  Give ``seq_lens`` the tensor of the
+    lengths themselves to step them in place."""
+
+    def __init__(self, B: int, n_tokens: int, device="cuda:0", seq_lens: Optional[torch.Tensor] = None):
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.cu_new, self.slots, self.positions, self.status = new(B + 1), new(n_tokens), new(n_tokens), new(B)
+        self.seq_lens = new(B) if seq_lens is None else seq_lens
+
+
+def vq_kv_pages_assign(new_lens: torch.Tensor, lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                       page_tokens: int, n_tokens: Optional[int] = None, plan: Optional[VQPagePlan] = None,
+                       n_free_out: Optional[torch.Tensor] = None) -> VQPagePlan:
+    """Pages for the new tokens of every request, and the pages of ended ones back: updates block_table, free_pages and
+    ``n_free_out`` (``n_free`` itself unless given), fills and returns ``plan`` (for ``n_tokens`` new tokens at most)."""
+    B = new_lens.shape[0]
+    if plan is None:
+        if n_tokens is None:
+            raise ValueError("n_tokens or a plan has to say how many new tokens the step can have")
+        plan = VQPagePlan(B, n_tokens, new_lens.device)
+    if n_free_out is None:
+        n_free_out = n_free
+    i32, tokens = torch.int32, plan.slots.shape[0]
+    if block_table.dim() != 2:
+        raise ValueError("block_table must have the shape (requests, pages)")
+    d = vq_page_step_t(B, block_table.shape[1], int(page_tokens), free_pages.shape[0], tokens,
+                       _here(new_lens, "new_lens", i32, (B,)), _here(lens, "lens", i32, (B,)), _here(block_table, "block_table", i32, (B, block_table.shape[1])),
+                       _here(free_pages, "free_pages", i32, (free_pages.shape[0],)), _here(n_free, "n_free", i32, (1,)),
+                       _here(plan.seq_lens, "seq_lens", i32, (B,)), _here(n_free_out, "n_free_out", i32, (1,)), _here(plan.cu_new, "cu_new", i32, (B + 1,)),
+                       _here(plan.slots, "slots", i32, (tokens,)), _here(plan.positions, "positions", i32, (tokens,)), _here(plan.status, "status", i32, (B,)))
+    _check(lib().vq_kv_pages_assign(ctypes.byref(d), _stream()), "vq_kv_pages_assign")
+    return plan
+
+
+def vq_kv_quantize_paged(kv: VQKVPagesDev, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantize new tokens (fp16 [tokens][H][D] each, tokens may lie apart) and store their codes at their slots (negative: skipped)."""
+    d = kv.desc()
+    kp, ks = _rows(k_new, "k_new", kv.H, kv.D)
+    vp, vs = _rows(v_new, "v_new", kv.H, kv.D)
+    n = k_new.shape[0]
+    _want(v_new, "v_new", tuple(k_new.shape))
+    _check(lib().vq_kv_quantize_paged(ctypes.byref(d), kp, ks, vp, vs, _here(slots, "slots", torch.int32, (n,)), n, _stream()),
+           "vq_kv_quantize_paged")
+
+
+def vq_attn_paged_workspace(kv: VQKVPagesDev, q: torch.Tensor, block_table: torch.Tensor) -> int:
+    """Workspace bytes of ``vq_attn_paged`` for queries and a block table of these shapes."""
+    d = kv.desc()
+    b = vq_paged_batch_t(block_table.shape[0], block_table.shape[1], q.shape[0], q.shape[1])
+    return int(lib().vq_attn_paged_workspace(ctypes.byref(d), ctypes.byref(b)))
+
+
+def vq_attn_paged(kv: VQKVPagesDev, q: torch.Tensor, sm_scale: float, block_table: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor,
+                  out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, window: int = 0, softcap: float = 0.0,
+                  slopes: Optional[torch.Tensor] = None, prefix_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[tokens][Hq][D]: attention of every request's new tokens (q, fp16, tokens may lie apart) over its pages, causal, optionally with
+    a sliding ``window``, capped scores, a distance bias and a prefix that all of them attend."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+    qp, qs = _rows(q, "q", None, kv.D)
+    op, os_ = _rows(out, "out", q.shape[1], kv.D)
+    _want(out, "out", tuple(q.shape))
+    if block_table.dim() != 2:
+        raise ValueError("block_table must have the shape (requests, pages)")
+    B, i32 = block_table.shape[0], torch.int32
+    b = vq_paged_batch_t(B, block_table.shape[1], q.shape[0], q.shape[1], _here(block_table, "block_table", i32), _here(cu_new, "cu_new", i32, (B + 1,)),
+                         _here(seq_lens, "seq_lens", i32, (B,)), _here(prefix_lens, "prefix_lens", i32, (B,)),
+                         _here(slopes, "slopes", torch.float32, (q.shape[1],)), int(window), float(softcap))
+    d, l = ctypes.byref(kv.desc()), lib()
+    ws_t, ws_p, ws_n = _workspace(q.device, ws, l.vq_attn_paged_workspace, d, ctypes.byref(b))
+    _check(l.vq_attn_paged(d, ctypes.byref(b), qp, qs, float(sm_scale), op, os_, ws_p, ws_n, _stream()), "vq_attn_paged")
     return out
 
 

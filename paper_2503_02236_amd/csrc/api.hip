@@ -1,5 +1,7 @@
 // C ABI of libvqmi: host-side argument validation and dispatch to the gfx950 kernels.
 // Operand format and operations: VQ-LLM (arXiv 2503.02236) Sec. II-A, II-B, III-C.
+#include <cfloat>
+#include <climits>
 #include <new>
 
 #include "vq_common.h"
@@ -49,6 +51,56 @@ int check_kv(const vq_kv_t *kv) {
         return VQ_ERR_ALIGN;
     if (kv->seq_lens && (reinterpret_cast<uintptr_t>(kv->seq_lens) & 3u)) return VQ_ERR_ALIGN;
     return VQ_OK;
+}
+
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+constexpr int kMostRequests = 65536, kMostTokens = 1 << 20;   // of a step
+
+// Sizes of a pool's pages.
+static bool page_sizes_ok(int n_pages, int page_tokens) {
+    return n_pages >= 0 && page_tokens >= 16 && page_tokens <= 256 && (page_tokens & (page_tokens - 1)) == 0 && (long long)n_pages * page_tokens <= INT_MAX;
+}
+
+int check_kv_pages(const vq_kv_pages_t *kv) {
+    if (!kv) return VQ_ERR_NULL;
+    vq_kv_t t{};   // (what the two caches have in common)
+    t.H = kv->H;
+    t.D = kv->D;
+    t.v = kv->v;
+    t.n_entries = kv->n_entries;
+    t.cb_groups = kv->cb_groups;
+    t.k_codes = kv->k_codes;
+    t.v_codes = kv->v_codes;
+    t.k_codebooks = kv->k_codebooks;
+    t.v_codebooks = kv->v_codebooks;
+    if (int st = check_kv(&t)) return st;
+    return page_sizes_ok(kv->n_pages, kv->page_tokens) ? VQ_OK : VQ_ERR_SHAPE;
+}
+
+static int check_page_step(const vq_page_step_t *p) {
+    if (!p) return VQ_ERR_NULL;
+    if (p->B < 0 || p->B > kMostRequests || p->max_pages < 1 || (long long)p->B * p->max_pages > INT_MAX || p->n_tokens < 0 || p->n_tokens > kMostTokens ||
+        !page_sizes_ok(p->n_pages, p->page_tokens) || (long long)p->max_pages * p->page_tokens > INT_MAX)
+        return VQ_ERR_SHAPE;
+    if (!p->n_free || !p->n_free_out || !p->cu_new || (!p->free_pages && p->n_pages > 0) || (!p->slots && p->n_tokens > 0) ||
+        (p->B > 0 && (!p->new_lens || !p->lens || !p->block_table || !p->seq_lens || !p->status)))
+        return VQ_ERR_NULL;
+    for (const void *q : {(const void *)p->new_lens, (const void *)p->lens, (const void *)p->block_table, (const void *)p->free_pages, (const void *)p->n_free,
+                          (const void *)p->seq_lens, (const void *)p->n_free_out, (const void *)p->cu_new, (const void *)p->slots, (const void *)p->positions,
+                          (const void *)p->status})
+        if (!aligned4(q)) return VQ_ERR_ALIGN;
+    return VQ_OK;
+}
+
+// Sizes only: what the workspace depends on.
+static int check_paged_sizes(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
+    if (int st = check_kv_pages(kv)) return st;
+    if (!b) return VQ_ERR_NULL;
+    if (kv->H < 1 || b->B < 0 || b->B > kMostRequests || b->max_pages < 1 || (long long)b->B * b->max_pages > INT_MAX ||
+        (long long)b->max_pages * kv->page_tokens > INT_MAX || b->n_tokens < 0 || b->n_tokens > kMostTokens || b->Hq < 1 || b->Hq % kv->H != 0 ||
+        (long long)b->n_tokens * (b->Hq / kv->H) > INT_MAX || b->window < 0 || !(b->softcap >= 0.f) || b->softcap > FLT_MAX)
+        return VQ_ERR_SHAPE;
+    return attn_paged_supported(kv) ? VQ_OK : VQ_ERR_UNSUPPORTED;
 }
 
 }  // namespace vq
@@ -484,6 +536,46 @@ int vq_kv_quantize(const vq_kv_t *kv, const void *k_new, const void *v_new, int 
     if (!aligned16(k_new) || !aligned16(v_new)) return VQ_ERR_ALIGN;
     if (n_new == 0 || kv->B == 0 || kv->H == 0) return VQ_OK;
     return launch_kv_quantize(kv, k_new, v_new, n_new, pos, static_cast<hipStream_t>(stream));
+}
+
+int vq_kv_pages_assign(const vq_page_step_t *step, void *stream) {
+    if (int st = check_page_step(step)) return st;
+    return launch_kv_pages_assign(step, static_cast<hipStream_t>(stream));
+}
+
+int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_stride, const void *v_new, size_t v_stride, const int *slots,
+                         int n_tokens, void *stream) {
+    int st = check_kv_pages(kv);
+    if (st != VQ_OK) return st;
+    if (n_tokens > 0 && (!k_new || !v_new || !slots)) return VQ_ERR_NULL;
+    const size_t row = (size_t)kv->H * kv->D;
+    if (n_tokens < 0 || n_tokens > kMostTokens || k_stride < row || v_stride < row || k_stride > (1u << 23) || v_stride > (1u << 23)) return VQ_ERR_SHAPE;
+    if (!aligned16(k_new) || !aligned16(v_new) || k_stride % 8 != 0 || v_stride % 8 != 0 || !aligned4(slots)) return VQ_ERR_ALIGN;
+    if (n_tokens == 0 || kv->H == 0) return VQ_OK;
+    return launch_kv_quantize_paged(kv, k_new, k_stride, v_new, v_stride, slots, n_tokens, static_cast<hipStream_t>(stream));
+}
+
+size_t vq_attn_paged_workspace(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch) {
+    if (check_paged_sizes(kv, batch) != VQ_OK) return 0;
+    return attn_paged_workspace(kv, batch);
+}
+
+int vq_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch, const void *q, size_t q_stride, float sm_scale, void *out,
+                  size_t out_stride, void *ws, size_t ws_bytes, void *stream) {
+    int st = check_paged_sizes(kv, batch);
+    if (st != VQ_OK) return st;
+    const bool empty = batch->B == 0 || batch->n_tokens == 0;
+    if (!empty && (!q || !out || !batch->block_table || !batch->cu_new || !batch->seq_lens)) return VQ_ERR_NULL;
+    const size_t row = (size_t)batch->Hq * kv->D;
+    if (q_stride < row || out_stride < row) return VQ_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(out) || q_stride % 8 != 0 || out_stride % 8 != 0 || !aligned4(batch->block_table) || !aligned4(batch->cu_new) ||
+        !aligned4(batch->seq_lens) || !aligned4(batch->prefix_lens) || !aligned4(batch->slopes))
+        return VQ_ERR_ALIGN;
+    if (empty) return VQ_OK;
+    const size_t need = attn_paged_workspace(kv, batch);
+    if (need && (!ws || ws_bytes < need)) return VQ_ERR_WORKSPACE;
+    if (ws && !aligned16(ws)) return VQ_ERR_ALIGN;
+    return launch_attn_paged(kv, batch, q, q_stride, sm_scale, out, out_stride, ws, static_cast<hipStream_t>(stream));
 }
 
 int vq_dequant(const vq_weight_t *w, void *W, int out_fp32, void *stream) {

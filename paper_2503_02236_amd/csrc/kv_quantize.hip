@@ -27,7 +27,19 @@ struct KvQuantArgs {
     unsigned pg_inverse;   // kvq_inverse(PG) (matrix-core kernel)
     int log_lanes;         // lanes that share an item (kv_quantize_lane_kernel)
     int share;             // workgroups that share a token range (kv_quantize_scan_kernel)
+    // PAGED kernels: x is [n_new][stride] with head h at h * D, one "sequence" of all requests' new tokens; codes go to slots
+    size_t stride[2];
+    const int *slots;      // [n_new]
+    int n_slots, log_ps;
 };
+
+// First code of a slot's head and side in the pages; sub-vector p lies kvq_pitch(side) * p behind it.
+__device__ __forceinline__ uint8_t *kvq_slot(const KvQuantArgs &a, int side, int h, unsigned slot) {
+    const unsigned off = slot & ((1u << a.log_ps) - 1u);
+    uint8_t *page = a.codes[side] + (((size_t)(slot >> a.log_ps) * a.H + h) * a.P << a.log_ps);
+    return page + (side ? (off & ~15u) * a.P + (off & 15u) : off * a.P);
+}
+__device__ __forceinline__ int kvq_pitch(int side) { return side ? 16 : 1; }
 
 // A sub-vector (V halves, aligned) in the low halves of 16 bytes, the rest zero.
 template <int V>
@@ -100,15 +112,16 @@ __device__ __forceinline__ int kvq_wave_argmin(float d, int e) {
 // Bound: the latency of two dependent loads and, per sub-vector, four distances and one reduction over the lanes.  One
 // token of B3 H32 with 32 codebooks per head and side: 4.4 us (5.3 with a workgroup per
 // token range), where staging both sides' codebooks in LDS took 14.7.  SHARED: several workgroups share a token range.
-template <int V, bool SHARED>
+template <int V, bool SHARED, bool PAGED>
 __global__ __launch_bounds__(512) void kv_quantize_scan_kernel(KvQuantArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     constexpr int NW = 8;
     const int bh = blockIdx.x, h = bh % a.H, side = SHARED ? blockIdx.z & 1 : blockIdx.z;
     const int t0 = blockIdx.y * a.tokens, nt = min(a.tokens, a.n_new - t0);
     const half_t *src = a.cb[side] + (size_t)h * a.G * a.E * V;
-    const half_t *xs = a.x[side] + ((size_t)bh * a.n_new + t0) * a.D;
-    uint8_t *dst = a.codes[side] + ((size_t)bh * a.T + a.pos + t0) * a.P;
+    const size_t stride = PAGED ? a.stride[side] : (size_t)a.D;
+    const half_t *xs = PAGED ? a.x[side] + t0 * stride + (size_t)h * a.D : a.x[side] + ((size_t)bh * a.n_new + t0) * a.D;
+    uint8_t *dst = PAGED ? nullptr : a.codes[side] + ((size_t)bh * a.T + a.pos + t0) * a.P;
     const int n_items = nt * a.PG;                // per group
     const int all = SHARED ? NW * a.share : NW;   // wavefronts of the workgroups that share these tokens
     const int R = max(1, all / a.G);              // wavefronts that share a group
@@ -119,7 +132,8 @@ __global__ __launch_bounds__(512) void kv_quantize_scan_kernel(KvQuantArgs a) {
         for (int k = 0; k < 4; ++k) c[k] = kvq_load<V>(src + ((size_t)g * a.E + min(lane + 64 * k, a.E - 1)) * V);
         for (int i = u % R; i < n_items; i += R) {
             const int t = i / a.PG, p = g * a.PG + (i - t * a.PG);
-            const V16 x = kvq_load<V>(xs + (size_t)t * a.D + p * V);   // the same for all lanes
+            const V16 x = kvq_load<V>(xs + t * stride + p * V);   // the same for all lanes
+            const int slot = PAGED ? a.slots[t0 + t] : 0;
             float bd = INFINITY;
             int be = lane;                        // (nothing is closer than infinity: entry 0, as lane 0 has it)
 #pragma unroll
@@ -130,7 +144,11 @@ __global__ __launch_bounds__(512) void kv_quantize_scan_kernel(KvQuantArgs a) {
                 bd = closer ? d : bd;
             }
             const int code = kvq_wave_argmin(bd, be);
-            if (lane == 0) dst[(size_t)t * a.P + p] = (uint8_t)code;
+            if constexpr (PAGED) {
+                if (lane == 0 && (unsigned)slot < (unsigned)a.n_slots) kvq_slot(a, side, h, slot)[p * kvq_pitch(side)] = (uint8_t)code;
+            } else {
+                if (lane == 0) dst[(size_t)t * a.P + p] = (uint8_t)code;
+            }
         }
     }
 }
@@ -140,7 +158,7 @@ __global__ __launch_bounds__(512) void kv_quantize_scan_kernel(KvQuantArgs a) {
 // 2^log_lanes-th entry.  Groups lie an entry more than their length apart, so that lanes of different groups read different
 // banks.  Bound: vector issue, about 4 + 2.5 V instructions per (item, entry); the matrix-core kernel spends 100 or more on
 // an item whatever E is.
-template <int V, int TOK>
+template <int V, int TOK, bool PAGED>
 __global__ __launch_bounds__(256) void kv_quantize_lane_kernel(KvQuantArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     half_t *cb = reinterpret_cast<half_t *>(smem);   // [G][E + 1][V]
@@ -148,8 +166,17 @@ __global__ __launch_bounds__(256) void kv_quantize_lane_kernel(KvQuantArgs a) {
     const int bh = blockIdx.x, h = bh % a.H, side = blockIdx.z;
     const int t0 = blockIdx.y * a.tokens, nt = min(a.tokens, a.n_new - t0);
     const half_t *src = a.cb[side] + (size_t)h * a.G * a.E * V;
-    const half_t *xs = a.x[side] + ((size_t)bh * a.n_new + t0) * a.D;
-    uint8_t *dst = a.codes[side] + ((size_t)bh * a.T + a.pos + t0) * a.P;
+    const size_t stride = PAGED ? a.stride[side] : (size_t)a.D;
+    const half_t *xs = PAGED ? a.x[side] + t0 * stride + (size_t)h * a.D : a.x[side] + ((size_t)bh * a.n_new + t0) * a.D;
+    uint8_t *dst = PAGED ? nullptr : a.codes[side] + ((size_t)bh * a.T + a.pos + t0) * a.P;
+    auto store = [&](int t, int p, int code) {
+        if constexpr (PAGED) {
+            const int slot = a.slots[t0 + t];
+            if ((unsigned)slot < (unsigned)a.n_slots) kvq_slot(a, side, h, slot)[p * kvq_pitch(side)] = (uint8_t)code;
+        } else {
+            dst[(size_t)t * a.P + p] = (uint8_t)code;
+        }
+    };
     for (int i = tid; i < a.G * a.E; i += 256) {
         const V16 c = kvq_load<V>(src + (size_t)i * V);
 #pragma unroll
@@ -166,7 +193,7 @@ __global__ __launch_bounds__(256) void kv_quantize_lane_kernel(KvQuantArgs a) {
             int be[TOK];
 #pragma unroll
             for (int k = 0; k < TOK; ++k) {
-                x[k] = kvq_load<V>(xs + (size_t)min(t + k * rows, nt - 1) * a.D + p * V);
+                x[k] = kvq_load<V>(xs + min(t + k * rows, nt - 1) * stride + p * V);
                 bd[k] = INFINITY;
                 be[k] = 0;
             }
@@ -181,14 +208,14 @@ __global__ __launch_bounds__(256) void kv_quantize_lane_kernel(KvQuantArgs a) {
             }
 #pragma unroll
             for (int k = 0; k < TOK; ++k)
-                if (t + k * rows < nt) dst[(size_t)(t + k * rows) * a.P + p] = (uint8_t)be[k];
+                if (t + k * rows < nt) store(t + k * rows, p, be[k]);
         }
     } else {
         const int lanes = 1 << a.log_lanes, sub = tid & (lanes - 1), n_items = nt * a.P;
         // (all lanes of a wavefront stay to the end: they merge what they found)
         for (int i0 = 0; i0 < n_items; i0 += 256 >> a.log_lanes) {
             const int i = min(i0 + (tid >> a.log_lanes), n_items - 1), t = i / a.P, p = i - t * a.P;
-            const V16 x = kvq_load<V>(xs + (size_t)t * a.D + p * V);
+            const V16 x = kvq_load<V>(xs + t * stride + p * V);
             const half_t *grp = cb + (size_t)(p / a.PG) * (a.E + 1) * V;
             float bd = INFINITY;
             int be = sub;      // (nothing is closer than infinity: entry 0, as the first lane has it)
@@ -209,7 +236,7 @@ __global__ __launch_bounds__(256) void kv_quantize_lane_kernel(KvQuantArgs a) {
                 be = od < bd || (od == bd && oe < be) ? oe : be;
                 bd = od < bd ? od : bd;
             }
-            if (sub == 0 && i0 + (tid >> a.log_lanes) < n_items) dst[(size_t)t * a.P + p] = (uint8_t)be;
+            if (sub == 0 && i0 + (tid >> a.log_lanes) < n_items) store(t, p, be);
         }
     }
 }
@@ -268,7 +295,7 @@ __device__ __forceinline__ int closer_of_two_lanes(float d, int e) {
 // 32 items at a time.  kKvqOwn: 64 items at a time, each lane its own item.  kKvqNorms: the same by s once more, with the entries'
 // |c|^2 / 2 from LDS, and by the definition only where two entries of the group are too close (run_kvq_mfma chooses).
 enum { kKvqPair, kKvqOwn, kKvqNorms };
-template <int V, int TILES, int WAY>
+template <int V, int TILES, int WAY, bool PAGED>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) void kv_quantize_mfma_kernel(KvQuantArgs a) {
     constexpr int EP = 32 * TILES, STEP = WAY == kKvqPair ? 32 : 64;
     constexpr bool NORMS = WAY == kKvqNorms;
@@ -310,7 +337,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 
     float ninf;
     asm("s_mov_b32 %0, 0xff800000" : "=s"(ninf));
-    const unsigned char *xs = reinterpret_cast<const unsigned char *>(a.x[side] + ((size_t)bh * a.n_new + t0) * a.D);
+    const size_t stride = PAGED ? a.stride[side] : (size_t)a.D;
+    const unsigned char *xs = reinterpret_cast<const unsigned char *>(PAGED ? a.x[side] + t0 * stride + (size_t)h * a.D
+                                                                            : a.x[side] + ((size_t)bh * a.n_new + t0) * a.D);
+    const unsigned beyond = PAGED ? (unsigned)(stride / V) - (unsigned)a.P : 0u;   // sub-vectors between the tokens' heads in memory
     const int n_items = nt * a.PG, n_ct = (n_items + STEP - 1) / STEP;   // per group
     const int R = max(1, NW / a.G);                              // wavefronts that share a group
     for (int u = wave; u < a.G * R; u += NW) {
@@ -355,12 +385,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
             return __umul24(__umul24(i, a.pg_inverse) >> 21, (unsigned)(a.P - a.PG)) + i + (unsigned)(g * a.PG);   // (kvq_quotient)
         };
         auto lane_off = [&](int ct) { return item_off((unsigned)min(ct * STEP + lane % STEP, n_items - 1)); };
-        auto load_item = [&](unsigned off) { return kvq_load<V>(xs + off * (V * 2)); };
+        // (PAGED: the token is off / P, and a workgroup's tokens span less than 2^32 bytes)
+        auto load_item = [&](unsigned off, int ct) {
+            if constexpr (PAGED) off += __umul24(__umul24((unsigned)min(ct * STEP + lane % STEP, n_items - 1), a.pg_inverse) >> 21, beyond);
+            return kvq_load<V>(xs + off * (V * 2));
+        };
         unsigned off = lane_off(min(u % R, n_ct - 1));
-        V16 xb = load_item(off);
+        V16 xb = load_item(off, min(u % R, n_ct - 1));
         for (int ct = u % R; ct < n_ct; ct += R) {
             const unsigned off_next = lane_off(min(ct + R, n_ct - 1));
-            const V16 xnext = load_item(off_next);
+            const V16 xnext = load_item(off_next, min(ct + R, n_ct - 1));
             V16 bop[2];   // items 0 .. 31 and 32 .. 63
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -496,6 +530,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
         }
     }
     __syncthreads();
+    if constexpr (PAGED) {
+        // values: 16 tokens side by side, a byte each (consecutive slots are consecutive bytes); keys: rows of P bytes
+        const int *slots = a.slots + t0;
+        if (side) {
+            for (int i = tid; i < ((nt + 15) & ~15) * a.P; i += blockDim.x) {
+                const int t = (i / (16 * a.P)) * 16 + (i & 15), p = i / 16 % a.P;
+                const int slot = t < nt ? slots[t] : -1;
+                if ((unsigned)slot < (unsigned)a.n_slots) kvq_slot(a, 1, h, slot)[p * 16] = out[t * a.P + p];
+            }
+        } else if ((a.P & 3) == 0) {
+            for (int i = tid; i < nt * a.P / 4; i += blockDim.x) {
+                const int t = i / (a.P / 4), slot = slots[t];
+                if ((unsigned)slot < (unsigned)a.n_slots)
+                    reinterpret_cast<uint32_t *>(kvq_slot(a, 0, h, slot))[i - t * (a.P / 4)] = reinterpret_cast<const uint32_t *>(out)[i];
+            }
+        } else {
+            for (int i = tid; i < nt * a.P; i += blockDim.x) {
+                const int t = i / a.P, slot = slots[t];
+                if ((unsigned)slot < (unsigned)a.n_slots) kvq_slot(a, 0, h, slot)[i - t * a.P] = out[i];
+            }
+        }
+        return;
+    }
     uint8_t *dst = a.codes[side] + ((size_t)bh * a.T + a.pos + t0) * a.P;
     if ((a.P & 3) == 0) {
         for (int i = tid; i < nt * a.P / 4; i += blockDim.x)
@@ -631,22 +688,22 @@ KvqMfmaPlan kvq_mfma_plan(int bh, int P, int v, int E, int G, int n_new) {
     return p;
 }
 
-template <int V, int TILES, int WAY>
+template <int V, int TILES, int WAY, bool PAGED>
 int run_kvq_mfma_as(const KvQuantArgs &a, int bh, const KvqMfmaPlan &p, hipStream_t s) {
     static KernelSetup setup;
-    if (int st = kernel_setup(reinterpret_cast<const void *>(&kv_quantize_mfma_kernel<V, TILES, WAY>), p.lds, false, setup)) return st;
-    kv_quantize_mfma_kernel<V, TILES, WAY><<<dim3(bh, (a.n_new + a.tokens - 1) / a.tokens, 2), p.threads, p.lds, s>>>(a);
+    if (int st = kernel_setup(reinterpret_cast<const void *>(&kv_quantize_mfma_kernel<V, TILES, WAY, PAGED>), p.lds, false, setup)) return st;
+    kv_quantize_mfma_kernel<V, TILES, WAY, PAGED><<<dim3(bh, (a.n_new + a.tokens - 1) / a.tokens, 2), p.threads, p.lds, s>>>(a);
     return launch_status();
 }
 
-template <int V, int TILES>
+template <int V, int TILES, bool PAGED>
 int run_kvq_mfma(const KvQuantArgs &a, int bh, const KvqMfmaPlan &p, hipStream_t s) {
-    if (p.way == kKvqPair) return run_kvq_mfma_as<V, TILES, kKvqPair>(a, bh, p, s);
-    if (p.way == kKvqNorms) return run_kvq_mfma_as<V, TILES, kKvqNorms>(a, bh, p, s);
-    return run_kvq_mfma_as<V, TILES, kKvqOwn>(a, bh, p, s);
+    if (p.way == kKvqPair) return run_kvq_mfma_as<V, TILES, kKvqPair, PAGED>(a, bh, p, s);
+    if (p.way == kKvqNorms) return run_kvq_mfma_as<V, TILES, kKvqNorms, PAGED>(a, bh, p, s);
+    return run_kvq_mfma_as<V, TILES, kKvqOwn, PAGED>(a, bh, p, s);
 }
 
-template <int V>
+template <int V, bool PAGED>
 int run_kvq_lane(KvQuantArgs &a, int bh, hipStream_t s) {
     a.tokens = std::min(a.n_new, kQuantLaneTokens);
     a.log_lanes = kvq_log_lanes(a.tokens * a.P);
@@ -654,34 +711,34 @@ int run_kvq_lane(KvQuantArgs &a, int bh, hipStream_t s) {
     const size_t lds = (size_t)a.G * (a.E + 1) * V * sizeof(half_t);   // (below 64 KiB: kQuantLaneBytes)
     if constexpr (V <= 4)
         if (kvq_four_tokens(a.P, V, a.n_new)) {
-            kv_quantize_lane_kernel<V, 4><<<grid, 256, lds, s>>>(a);
+            kv_quantize_lane_kernel<V, 4, PAGED><<<grid, 256, lds, s>>>(a);
             return launch_status();
         }
-    kv_quantize_lane_kernel<V, 1><<<grid, 256, lds, s>>>(a);
+    kv_quantize_lane_kernel<V, 1, PAGED><<<grid, 256, lds, s>>>(a);
     return launch_status();
 }
 
-template <int V>
+template <int V, bool PAGED>
 int run_kvq(KvQuantArgs &a, int bh, hipStream_t s) {
     const int kernel = kvq_choice(bh, a.P, V, a.E, a.G, a.n_new);
-    if (kernel == kKvqLane) return run_kvq_lane<V>(a, bh, s);
+    if (kernel == kKvqLane) return run_kvq_lane<V, PAGED>(a, bh, s);
     if (kernel == kKvqScan) {
         a.tokens = std::min(a.n_new, kQuantScanTokens);
         const int ranges = ceil_div(a.n_new, a.tokens);
         a.share = kvq_share(bh, ranges, a.tokens * a.P);
         if (a.share > 1)
-            kv_quantize_scan_kernel<V, true><<<dim3(bh, ranges, 2 * a.share), 512, 0, s>>>(a);
+            kv_quantize_scan_kernel<V, true, PAGED><<<dim3(bh, ranges, 2 * a.share), 512, 0, s>>>(a);
         else
-            kv_quantize_scan_kernel<V, false><<<dim3(bh, ranges, 2), 512, 0, s>>>(a);
+            kv_quantize_scan_kernel<V, false, PAGED><<<dim3(bh, ranges, 2), 512, 0, s>>>(a);
         return launch_status();
     }
     a.pg_inverse = kvq_inverse(a.PG);
     const KvqMfmaPlan p = kvq_mfma_plan(bh, a.P, V, a.E, a.G, a.n_new);
     a.tokens = p.tokens;
-    if (a.E <= 32) return run_kvq_mfma<V, 1>(a, bh, p, s);
-    if (a.E <= 64) return run_kvq_mfma<V, 2>(a, bh, p, s);
-    if (a.E <= 128) return run_kvq_mfma<V, 4>(a, bh, p, s);
-    return run_kvq_mfma<V, 8>(a, bh, p, s);
+    if (a.E <= 32) return run_kvq_mfma<V, 1, PAGED>(a, bh, p, s);
+    if (a.E <= 64) return run_kvq_mfma<V, 2, PAGED>(a, bh, p, s);
+    if (a.E <= 128) return run_kvq_mfma<V, 4, PAGED>(a, bh, p, s);
+    return run_kvq_mfma<V, 8, PAGED>(a, bh, p, s);
 }
 
 }  // namespace
@@ -722,10 +779,42 @@ int launch_kv_quantize(const vq_kv_t *kv, const void *k_new, const void *v_new, 
     a.pos = pos;
     a.PG = a.P / a.G;
     a.pg_inverse = 0;
+    a.stride[0] = a.stride[1] = 0;
+    a.slots = nullptr;
+    a.n_slots = a.log_ps = 0;
     const int bh = kv->B * kv->H;
-    if (kv->v == 8) return run_kvq<8>(a, bh, s);
-    if (kv->v == 4) return run_kvq<4>(a, bh, s);
-    return run_kvq<2>(a, bh, s);
+    if (kv->v == 8) return run_kvq<8, false>(a, bh, s);
+    if (kv->v == 4) return run_kvq<4, false>(a, bh, s);
+    return run_kvq<2, false>(a, bh, s);
+}
+
+// All new tokens of a step as one sequence per head: the same kernels, choice and codes, other addresses.
+int launch_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_stride, const void *v_new, size_t v_stride, const int *slots,
+                             int n_tokens, hipStream_t s) {
+    const size_t cb_bytes = (size_t)kv->cb_groups * kv->n_entries * kv->v * sizeof(half_t);
+    if (cb_bytes > 64 * 1024 || cb_bytes % 16 != 0) return VQ_ERR_UNSUPPORTED;
+    KvQuantArgs a{};
+    a.x[0] = (const half_t *)k_new;
+    a.x[1] = (const half_t *)v_new;
+    a.stride[0] = k_stride;
+    a.stride[1] = v_stride;
+    a.cb[0] = (const half_t *)kv->k_codebooks;
+    a.cb[1] = (const half_t *)kv->v_codebooks;
+    a.codes[0] = (uint8_t *)const_cast<void *>(kv->k_codes);
+    a.codes[1] = (uint8_t *)const_cast<void *>(kv->v_codes);
+    a.H = kv->H;
+    a.D = kv->D;
+    a.P = kv->D / kv->v;
+    a.E = kv->n_entries;
+    a.G = kv->cb_groups;
+    a.n_new = n_tokens;
+    a.PG = a.P / a.G;
+    a.slots = slots;
+    a.n_slots = kv->n_pages * kv->page_tokens;
+    a.log_ps = __builtin_ctz(kv->page_tokens);
+    if (kv->v == 8) return run_kvq<8, true>(a, kv->H, s);
+    if (kv->v == 4) return run_kvq<4, true>(a, kv->H, s);
+    return run_kvq<2, true>(a, kv->H, s);
 }
 
 }  // namespace vq

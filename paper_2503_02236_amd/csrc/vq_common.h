@@ -148,6 +148,7 @@ void gemv_pipeline_destroy(GemvPipeline *h);
 int launch_gemv_pipeline(const GemvPipeline *h, hipStream_t s);
 int gemv_pipeline_status(const GemvPipeline *h, hipStream_t s, int *status);
 int check_kv(const vq_kv_t *kv);
+int check_kv_pages(const vq_kv_pages_t *kv);
 
 // Kernel launchers (defined next to their kernels).
 int launch_dequant(const vq_weight_t *w, void *W, int out_fp32, hipStream_t s);
@@ -201,6 +202,14 @@ size_t attn_channel_workspace(const vq_kv_t *kv);
 int launch_attn_channel(const vq_kv_t *kv, const void *q, float sm_scale, void *out, void *ws, hipStream_t s);
 size_t attn_decode_workspace(const vq_kv_t *kv);
 int launch_kv_quantize(const vq_kv_t *kv, const void *k_new, const void *v_new, int n_new, int pos, hipStream_t s);
+// the paged cache (pages.hip, kv_quantize.hip, attn_paged.hip)
+int launch_kv_pages_assign(const vq_page_step_t *step, hipStream_t s);
+int launch_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_stride, const void *v_new, size_t v_stride, const int *slots,
+                             int n_tokens, hipStream_t s);
+bool attn_paged_supported(const vq_kv_pages_t *kv);
+size_t attn_paged_workspace(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch);
+int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch, const void *q, size_t q_stride, float sm_scale, void *out,
+                      size_t out_stride, void *ws, hipStream_t s);
 int launch_probe_copy(void *dst, const void *src, size_t bytes, hipStream_t s);
 int launch_probe_read(const void *src, size_t bytes, void *sink, hipStream_t s);
 int launch_probe_mfma(int workgroups, int iters, int random_operands, void *sink, hipStream_t s);
