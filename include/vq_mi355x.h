@@ -422,7 +422,7 @@ typedef struct vq_kv_pages_t {
  */
 typedef struct vq_page_step_t {
     int B;                 /* requests; 0 <= B <= 65536 */
-    int max_pages;         /* row length of the block table, >= 1; B * max_pages < 2^31 */
+    int max_pages;         /* row length of the block table, >= 1; B * max_pages < 2^31, max_pages * page_tokens <= 2^30 */
     int page_tokens;       /* as in vq_kv_pages_t */
     int n_pages;           /* pages of the pool, n_pages * page_tokens < 2^31 */
     int n_tokens;          /* most new tokens of the step: length of slots and positions, 0 <= n_tokens <= 2^20 */
@@ -472,7 +472,7 @@ int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_st
  */
 typedef struct vq_paged_batch_t {
     int B;                   /* requests, 0 <= B <= 65536 */
-    int max_pages;           /* row length of the block table, >= 1; B * max_pages < 2^31; max_pages * page_tokens < 2^31 */
+    int max_pages;           /* row length of the block table, >= 1; B * max_pages < 2^31, max_pages * page_tokens <= 2^30 */
     int n_tokens;            /* rows of q and out: cu_new[B] or more, 0 <= n_tokens <= 2^20 */
     int Hq;                  /* query heads, a multiple of H */
     const int *block_table;  /* device, int32 [B][max_pages] */

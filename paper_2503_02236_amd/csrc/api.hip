@@ -54,7 +54,7 @@ int check_kv(const vq_kv_t *kv) {
 }
 
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-constexpr int kMostRequests = 65536, kMostTokens = 1 << 20;   // of a step
+constexpr int kMostRequests = 65536, kMostTokens = 1 << 20, kMostLength = 1 << 30;   // of a step; tokens of a row of the block table
 
 // Sizes of a pool's pages.
 static bool page_sizes_ok(int n_pages, int page_tokens) {
@@ -80,7 +80,7 @@ int check_kv_pages(const vq_kv_pages_t *kv) {
 static int check_page_step(const vq_page_step_t *p) {
     if (!p) return VQ_ERR_NULL;
     if (p->B < 0 || p->B > kMostRequests || p->max_pages < 1 || (long long)p->B * p->max_pages > INT_MAX || p->n_tokens < 0 || p->n_tokens > kMostTokens ||
-        !page_sizes_ok(p->n_pages, p->page_tokens) || (long long)p->max_pages * p->page_tokens > INT_MAX)
+        !page_sizes_ok(p->n_pages, p->page_tokens) || (long long)p->max_pages * p->page_tokens > kMostLength)
         return VQ_ERR_SHAPE;
     if (!p->n_free || !p->n_free_out || !p->cu_new || (!p->free_pages && p->n_pages > 0) || (!p->slots && p->n_tokens > 0) ||
         (p->B > 0 && (!p->new_lens || !p->lens || !p->block_table || !p->seq_lens || !p->status)))
@@ -97,7 +97,7 @@ static int check_paged_sizes(const vq_kv_pages_t *kv, const vq_paged_batch_t *b)
     if (int st = check_kv_pages(kv)) return st;
     if (!b) return VQ_ERR_NULL;
     if (kv->H < 1 || b->B < 0 || b->B > kMostRequests || b->max_pages < 1 || (long long)b->B * b->max_pages > INT_MAX ||
-        (long long)b->max_pages * kv->page_tokens > INT_MAX || b->n_tokens < 0 || b->n_tokens > kMostTokens || b->Hq < 1 || b->Hq % kv->H != 0 ||
+        (long long)b->max_pages * kv->page_tokens > kMostLength || b->n_tokens < 0 || b->n_tokens > kMostTokens || b->Hq < 1 || b->Hq % kv->H != 0 ||
         (long long)b->n_tokens * (b->Hq / kv->H) > INT_MAX || b->window < 0 || !(b->softcap >= 0.f) || b->softcap > FLT_MAX)
         return VQ_ERR_SHAPE;
     return attn_paged_supported(kv) ? VQ_OK : VQ_ERR_UNSUPPORTED;

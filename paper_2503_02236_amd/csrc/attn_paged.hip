@@ -1,5 +1,29 @@
 // Attention of the new tokens of a batch of requests over a paged cache of VQ codes (vq_attn_paged).
+//
+// Mathematics.  For a cache head h the rows are (new token, query head of the group).  A wavefront takes 32 rows and walks over
+// tiles of 32 cached tokens with the running maximum m, sum l and accumulators of a softmax:
+//   S^T = K Q^T   v_mfma_f32_32x32x16_f16, operand A = K: lane (key, half) takes 8 channels of its key, gathered by code from the
+//                 codebook in LDS straight into the operand.  Which key a row of the operand is, and which channel a step, is free: row
+//                 16 s + 8 a + 4 l + j is key 16 s + 8 l + 4 a + j, and half l takes the channels of its half of the head, so that a lane's codes are
+//                 consecutive bytes and its scores are those of the keys 16 s + 8 l + (0 .. 7) of one row;
+//   O^T = V^T P^T with P^T as operand B: exactly those scores, after exp2, as halves: no shuffle, no LDS.  Operand A = V^T: the lane
+//                 takes the channels of one position for its 8 keys (8 consecutive bytes of codes: the layout of the value pages), and
+//                 permutes the gathered pairs into D / 32 operands.
+// A weight is 2^(s - m + 6) rounded to a half (relative error 2^-11; the sum l takes it unrounded): m follows the maximum only when
+// that has grown by more than 8, so weights lie below 2^14 and those that fall below a half's range are below 2^-31 of the largest.
+// Sums, statistics and outputs before the last rounding are fp32.
+//
+// Codebooks in LDS (64 KiB a side).  V: row e holds entry e for all 32 channel positions of the operand, so the 32 lanes of a pass
+// read 32 different columns: no bank conflicts, whatever the codebook groups.  K: one codebook per head: every entry
+// 256 / (2 v) times in a row of 256 bytes, lane l reads copy l, again without conflicts; more: a table per sub-vector.
+//
+// Work.  A workgroup of 8 wavefronts (one per compute unit, for its LDS) belongs to a cache head and takes an equal share of the head's
+// work.  A request's rows are cut into blocks of 256 / ways rows; in a block `ways` wavefronts share 32 rows and take every ways-th tile of keys
+// (a round: one tile per wavefront), so that few rows fill the workgroup and many are not joined at the end.  Blocks of a request go in pairs (the last with the
+// first, ...), whose rounds add up to nearly the same number C: the work before a block is a product, not a sum, and every workgroup finds its share
+// with one scan over the requests.  A block cut by a share's border leaves its sums in ws, and attn_paged_merge_kernel joins them in order.
 #include <cfloat>
+#include <climits>
 
 #include "vq_common.h"
 
@@ -7,7 +31,14 @@ namespace vq {
 
 namespace {
 
-
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaves = 8, kThreads = kWaves * 64;
+constexpr int kSide = 65536;                  // LDS of a side's codebooks
+constexpr int kJoinOff = 2 * kSide;           // sums of wavefronts that share rows, 2 KiB each
+constexpr int kStatOff = kJoinOff + 16384;    // their maxima and sums of weights, [wave][32] each
+constexpr int kScanOff = kStatOff + 2048;
+constexpr int kLds = kScanOff + 256;
+constexpr float kHeadroom = 6.f, kRise = 8.f; // (log2)
 
 struct PagedArgs {
     const uint8_t *k_codes, *v_codes;
@@ -16,58 +47,658 @@ struct PagedArgs {
     const float *slopes;
     const half_t *q;
     half_t *out;
+    float *ws;
     size_t q_stride, out_stride;
-    int B, H, group, E, G, n_pages, max_pages, log_ps, n_tokens, window;
-    float scale, softcap;
+    int B, H, group, E, G, pg_shift, n_pages, max_pages, log_ps, n_tokens, window;
+    int workers;        // workgroups of a cache head
+    int min_log_ways;   // fewest wavefronts that share 32 rows
+    int cut;            // 0: blocks are not cut
+    int min_share;      // rounds
+    float scale2;       // |sm_scale| log2(e)
+    unsigned q_sign;    // sign of sm_scale, in both halves
+    float cap_in, cap_out;   // softcap: cap_out - 2 cap_out / (2^(s cap_in) + 1), 0: none
 };
 
-// A wavefront per new token and query head; a lane per channel pair, keys one after the other.
-template <int D>
-__global__ __launch_bounds__(64) void attn_paged_row_kernel(PagedArgs a, int V) {
-    const int lane = threadIdx.x, row = blockIdx.x, hq = blockIdx.y, h = hq / a.group;
-    if (row >= min(a.cu_new[a.B], a.n_tokens)) return;
-    int lo = 0, hi = a.B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (a.cu_new[mid + 1] > row) hi = mid;
-        else lo = mid + 1;
+// A request, in numbers that fit no memory access out of bounds.
+struct Request {
+    int first, n, len, prefix, rows, log_ways, blocks, items, C;
+};
+// Tiles of 32 keys that some of the tokens [i0, i1] attends: [0, front) and [lo, hi).
+struct Tiles {
+    int front, lo, hi;
+    __device__ int count() const { return front + max(hi - lo, 0); }
+};
+__device__ __forceinline__ Tiles tiles_of(const PagedArgs &a, const Request &r, int i0, int i1) {
+    const int p0 = r.len - r.n + i0, p1 = r.len - r.n + i1;
+    Tiles t;
+    t.lo = (a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0) >> 5;
+    t.hi = (max(p1 + 1, r.prefix) + 31) >> 5;
+    t.front = min((r.prefix + 31) >> 5, t.lo);
+    return t;
+}
+__device__ __forceinline__ int block_rows(const Request &r) { return (kWaves * 32) >> r.log_ways; }
+__device__ __forceinline__ Tiles block_tiles(const PagedArgs &a, const Request &r, int j) {
+    const int row = j * block_rows(r);
+    return tiles_of(a, r, row / a.group, (min(row + block_rows(r), r.rows) - 1) / a.group);
+}
+__device__ __forceinline__ int block_rounds(const PagedArgs &a, const Request &r, int j) {   // (a block that attends nothing writes zeros)
+    return max((block_tiles(a, r, j).count() + (1 << r.log_ways) - 1) >> r.log_ways, 1);
+}
+__device__ __forceinline__ Request request_of(const PagedArgs &a, int b) {
+    Request r;
+    const int c0 = min(max(a.cu_new[b], 0), a.n_tokens), c1 = min(max(a.cu_new[b + 1], 0), a.n_tokens);
+    r.first = c0;
+    r.n = max(c1 - c0, 0);
+    r.len = a.n_pages > 0 ? min(max(a.seq_lens[b], 0), a.max_pages << a.log_ps) : 0;
+    r.prefix = a.prefix_lens ? min(max(a.prefix_lens[b], 0), r.len) : 0;
+    r.rows = r.n * a.group;
+    r.log_ways = max(r.rows <= 32 ? 3 : r.rows <= 64 ? 2 : r.rows <= 128 ? 1 : 0, a.min_log_ways);
+    r.blocks = (r.rows + block_rows(r) - 1) / block_rows(r);
+    r.items = (r.blocks + 1) / 2;
+    r.C = r.blocks == 0 ? 0 : block_rounds(a, r, 0);
+    if (r.blocks > 1) r.C = max(r.C + block_rounds(a, r, r.blocks - 1), 2 * block_rounds(a, r, r.blocks / 2)) + 1;
+    return r;
+}
+
+// The share of worker w: rounds [u0, u1) of the head's, the first of them round x of request b.  False: none.  All threads of the
+// workgroup call it; xs: LDS, threads / 64 + 2 values.
+struct Share {
+    long long u0, u1, share, x;
+    int b;
+};
+template <int THREADS>
+__device__ __forceinline__ bool find_share(const PagedArgs &a, int w, long long *xs, Share *out) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int NW = THREADS / 64;
+    long long mine = 0, total = 0, own = 0;
+    for (int b = tid; b < a.B; b += THREADS) {
+        const Request r = request_of(a, b);
+        own = (long long)r.items * r.C;
+        mine += own;
     }
-    const int b = lo, ps = 1 << a.log_ps, P = D / V, PG = P / a.G;
-    const int len = a.n_pages > 0 ? min(max(a.seq_lens[b], 0), a.max_pages << a.log_ps) : 0;
-    const int pos = len - (a.cu_new[b + 1] - row);
-    const int prefix = a.prefix_lens ? a.prefix_lens[b] : 0;
-    constexpr int C = D / 64;
-    float q[C], o[C], m = -FLT_MAX, l = 0.f;
+    long long incl = mine;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        q[c] = (float)a.q[(size_t)row * a.q_stride + (size_t)hq * D + lane * C + c];
-        o[c] = 0.f;
+    for (int d = 1; d < 64; d <<= 1) {
+        const long long y = __shfl_up(incl, d, 64);
+        if (lane >= d) incl += y;
     }
-    for (int t = 0; t < len; ++t) {
-        if (!((t <= pos && (a.window == 0 || t > pos - a.window)) || t < prefix)) continue;
-        const int page = min(max(a.table[(size_t)b * a.max_pages + (t >> a.log_ps)], 0), a.n_pages - 1), off = t & (ps - 1);
-        const size_t base = ((size_t)page * a.H + h) * ps * P;
-        float k[C], v[C], s = 0.f;
+    if (lane == 63) xs[wave] = incl;
+    __syncthreads();
+    long long before = 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int ch = lane * C + c, p = ch / V, i = ch % V, g = p / PG;
-            const int kc = min((int)a.k_codes[base + (size_t)off * P + p], a.E - 1);
-            const int vc = min((int)a.v_codes[base + (size_t)(off / 16) * P * 16 + p * 16 + off % 16], a.E - 1);
-            k[c] = (float)a.k_cb[(((size_t)h * a.G + g) * a.E + kc) * V + i];
-            v[c] = (float)a.v_cb[(((size_t)h * a.G + g) * a.E + vc) * V + i];
-            s += q[c] * k[c];
+    for (int i = 0; i < NW; ++i) {
+        if (i < wave) before += xs[i];
+        total += xs[i];
+    }
+    incl += before;
+    out->share = max((total + a.workers - 1) / a.workers, (long long)a.min_share);
+    out->u0 = w * out->share;
+    out->u1 = min(out->u0 + out->share, total);
+    if (out->u0 >= total) return false;
+    __syncthreads();
+    if (a.B <= THREADS) {
+        if (incl - mine <= out->u0 && out->u0 < incl) {
+            xs[NW] = tid;
+            xs[NW + 1] = out->u0 - (incl - mine);
         }
-        s = wave_sum(s) * a.scale;
-        if (a.softcap > 0.f) s = a.softcap * tanhf(s / a.softcap);
-        if (a.slopes) s -= a.slopes[hq] * fabsf((float)(pos - t));
-        const float m_new = fmaxf(m, s), f = expf(m - m_new), p = expf(s - m_new);
-        m = m_new;
-        l = l * f + p;
+    } else {
+        long long carry = 0;
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+            const int b = b0 + tid;
+            long long u = 0;
+            if (b < a.B) {
+                const Request r = request_of(a, b);
+                u = (long long)r.items * r.C;
+            }
+            long long in = u, chunk = 0, lower = 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = o[c] * f + p * v[c];
+            for (int d = 1; d < 64; d <<= 1) {
+                const long long y = __shfl_up(in, d, 64);
+                if (lane >= d) in += y;
+            }
+            if (lane == 63) xs[wave] = in;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                if (i < wave) lower += xs[i];
+                chunk += xs[i];
+            }
+            __syncthreads();
+            const long long from = carry + lower + in - u;
+            if (from <= out->u0 && out->u0 < from + u) {
+                xs[NW] = b;
+                xs[NW + 1] = out->u0 - from;
+            }
+            carry += chunk;
+        }
+    }
+    __syncthreads();
+    const long long b = xs[NW], x = xs[NW + 1];
+    out->b = __builtin_amdgcn_readfirstlane((int)b);
+    out->x = ((long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+    return true;
+}
+
+// Sums of cut blocks: two per worker (the block that its share begins inside, the one that it ends inside), [rows][D] and [rows][2].
+__device__ __forceinline__ size_t part_of(const PagedArgs &a, int h, int w, int which) { return ((size_t)h * a.workers + w) * 2 + which; }
+__device__ __forceinline__ int part_rows(const PagedArgs &a) { return (kWaves * 32) >> a.min_log_ways; }
+template <int D>
+__device__ __forceinline__ float *part_sums(const PagedArgs &a, size_t part) { return a.ws + part * part_rows(a) * D; }
+template <int D>
+__device__ __forceinline__ float *part_stats(const PagedArgs &a, size_t part) {
+    return a.ws + (size_t)a.H * a.workers * 2 * part_rows(a) * D + part * part_rows(a) * 2;
+}
+
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<16> { typedef unsigned type __attribute__((ext_vector_type(4))); };
+template <>
+struct Raw<8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
+template <>
+struct Raw<4> { typedef unsigned type; };
+
+// BYTES from an LDS byte address to dwords
+template <int BYTES>
+__device__ __forceinline__ void lds_read(unsigned addr, uint32_t *to) {
+    typedef typename Raw<BYTES>::type raw_t;
+    const raw_t r = *reinterpret_cast<const __attribute__((address_space(3))) raw_t *>((uintptr_t)addr);
+    __builtin_memcpy(to, &r, BYTES);
+}
+template <int BYTES>
+__device__ __forceinline__ typename Raw<BYTES>::type global_read(const void *p) {
+    return *reinterpret_cast<const typename Raw<BYTES>::type *>(p);
+}
+
+// byte B of w in bits 8 .. 15, the lane's constant around it
+template <int B>
+__device__ __forceinline__ unsigned row_address(uint32_t w, unsigned lane_const) {
+    return __builtin_amdgcn_perm(w, lane_const, 0x0c020000u | ((4u + B) << 8));
+}
+
+// Codebooks of head h to LDS.  Rows of entries that do not exist are zero.
+template <int D, int V, bool COPIES>
+__device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned char *smem, int tid) {
+    constexpr int ES = 2 * V, P = D / V;
+    const unsigned char *kc = reinterpret_cast<const unsigned char *>(a.k_cb) + (size_t)h * a.G * a.E * ES;
+    const unsigned char *vc = reinterpret_cast<const unsigned char *>(a.v_cb) + (size_t)h * a.G * a.E * ES;
+    typedef typename Raw<ES>::type entry_t;
+    const entry_t none = {};
+    if constexpr (COPIES) {
+        constexpr int N = 256 * 16 / kThreads;      // units of 16 bytes
+        entry_t e[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = (tid + i * kThreads) >> 4;
+            e[i] = row < a.E ? global_read<ES>(kc + (size_t)row * ES) : none;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            entry_t r[16 / ES];
+#pragma unroll
+            for (int k = 0; k < 16 / ES; ++k) r[k] = e[i];
+            uint4 u;
+            __builtin_memcpy(&u, r, 16);
+            reinterpret_cast<uint4 *>(smem)[tid + i * kThreads] = u;
+        }
+    } else {
+        constexpr int N = P * 256 / kThreads;
+        entry_t e[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int u = tid + i * kThreads, row = u & 255, p = u >> 8;
+            e[i] = row < a.E ? global_read<ES>(kc + ((size_t)(p >> a.pg_shift) * a.E + row) * ES) : none;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(smem)[tid + i * kThreads] = e[i];
+    }
+    constexpr int CH = D / 32, US = 2 * (V < CH ? V : CH), UNITS = 2 * D / US;   // parts of an entry that one lane takes
+    constexpr int N = 256 * UNITS / kThreads;
+    typedef typename Raw<US>::type unit_t;
+    const unit_t zero = {};
+    unit_t e[N];
+    auto place = [&](int i, int *row, int *unit) {
+        const int u = tid + i * kThreads;
+        if (COPIES) {   // neighbours read one entry
+            *row = u / UNITS;
+            *unit = u % UNITS;
+        } else {        // eight entries of eight positions: 64-byte pieces from memory, eight columns of LDS
+            *row = (u >> 3) / UNITS * 8 + (u & 7);
+            *unit = (u >> 3) % UNITS;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        int row, unit;
+        place(i, &row, &unit);
+        const int ch = unit * (US / 2), p = ch / V;
+        e[i] = row < a.E ? global_read<US>(vc + ((size_t)(p >> a.pg_shift) * a.E + row) * ES + (ch % V) * 2) : zero;
     }
 #pragma unroll
-    for (int c = 0; c < C; ++c) a.out[(size_t)row * a.out_stride + (size_t)hq * D + lane * C + c] = (half_t)(l == 0.f ? 0.f : o[c] / l);
+    for (int i = 0; i < N; ++i) {
+        int row, unit;
+        place(i, &row, &unit);
+        *reinterpret_cast<unit_t *>(smem + kSide + row * 256 + unit * US) = e[i];
+    }
+}
+
+template <int D, int V, bool COPIES, bool MODS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_paged_kernel(PagedArgs a) {
+    constexpr int P = D / V, ES = 2 * V;
+    constexpr int CH = D / 32;                   // channels per lane of an operand V^T
+    constexpr int NC = D / 16;                   // steps of the product with K
+    constexpr int KW = P / 8;                    // dwords of a lane's K codes: half a token's
+    constexpr int CPS = 8 / V;                   // K codes of a step
+    constexpr int NSV = CH > V ? CH / V : 1;     // positions of a lane's V channels
+    constexpr int VR = 2 * (V < CH ? V : CH);    // bytes of a gather
+    constexpr int NB = V == 2 ? 2 : 4;           // tiles of codes in flight
+    constexpr int NG = D / 16;                   // groups of eight accumulators
+    extern __shared__ __align__(16) unsigned char smem[];   // (from LDS address 0: kernel_setup checks that)
+    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // consecutive workers of a head on one die: its codebooks and codes in one L2
+    const int nwg = gridDim.x, id = (nwg & 7) == 0 ? (int)(blockIdx.x & 7) * (nwg >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+    const int h = id / a.workers, w = id - h * a.workers;
+
+    Share sh;
+    if (!find_share<kThreads>(a, w, reinterpret_cast<long long *>(smem + kScanOff), &sh)) return;
+    stage_tables<D, V, COPIES>(a, h, smem, tid);
+    __syncthreads();
+
+    const int ps_mask = (1 << a.log_ps) - 1;
+    // lane constants of the gathers
+    const unsigned k_const = COPIES ? (unsigned)((V == 2 ? lane : V == 4 ? ln : ln & 15) * ES) : (unsigned)(lh * (P / 2) * 256 * ES);
+    const unsigned v_const = (unsigned)kSide + (unsigned)(ln * CH * 2);
+    // offsets of the lane's codes in a block of 16 tokens
+    const int key16 = 8 * ((ln >> 2) & 1) + 4 * ((ln >> 3) & 1) + (ln & 3);
+    const unsigned k_off = (unsigned)(key16 * P + lh * (P / 2)), v_off = (unsigned)(ln * CH / V * 16 + lh * 8);
+    float *xs = reinterpret_cast<float *>(smem + kJoinOff), *xm = reinterpret_cast<float *>(smem + kStatOff), *xl = xm + kWaves * 32;
+
+    // rounds [r0, r1) of block j of request r
+    auto run_block = [&](const Request &r, int b, int j, int r0, int r1, int rounds) {
+        const int ways = 1 << r.log_ways, rt = wave >> r.log_ways, kw = wave & (ways - 1);
+        const int row0 = j * block_rows(r) + rt * 32, tile_rows = min(r.rows - row0, 32);
+        const Tiles bt = block_tiles(a, r, j);
+        const bool valid = ln < tile_rows;
+        const int row = valid ? row0 + ln : min(row0, r.rows - 1), i = row / a.group, hq = h * a.group + (row - i * a.group);
+        const int pos = r.len - r.n + i;
+
+        float16_t o[CH];
+#pragma unroll
+        for (int f = 0; f < CH; ++f)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
+        float m_ref = -FLT_MAX, lsum = 0.f;
+
+        const int i0 = row0 / a.group, i1 = (row0 + tile_rows - 1) / a.group;
+        const int count = tile_rows > 0 ? bt.front + max(min(tiles_of(a, r, i0, i1).hi, bt.hi) - bt.lo, 0) : 0;
+        const int idx0 = r0 * ways + kw, idx_end = min(r1 * ways, count);
+        const int steps = idx0 < idx_end ? (idx_end - idx0 + ways - 1) >> r.log_ways : 0;
+        if (steps > 0) {
+            const int pos_f = r.len - r.n + i0, pos_l = r.len - r.n + i1;
+            half8_t qf[NC];
+            {
+                const half_t *qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)hq * D + lh * (D / 2);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    V16 u = ld16(qp + 8 * c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u.w[e] ^= a.q_sign;
+                    qf[c] = u.h8;
+                }
+            }
+            const float slope2 = MODS && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
+            const int see_to = min(pos, r.len - 1), see_from = a.window > 0 ? pos - a.window + 1 : INT_MIN;
+
+            auto tile_at = [&](int step) {
+                const int idx = min(idx0 + (step << r.log_ways), idx_end - 1);
+                return idx < bt.front ? idx : bt.lo + idx - bt.front;
+            };
+            // Pages of 32 steps at a time: lane 2 s + k holds the first byte of the codes of block k of step s.
+            auto page_ids = [&](int step) {
+                const int t = min(tile_at(step + (lane >> 1)) * 32 + 16 * (lane & 1), r.len - 1);
+                return a.table[(size_t)b * a.max_pages + (t >> a.log_ps)];
+            };
+            auto block_base = [&](int step, int pid) {
+                const int t = tile_at(step + (lane >> 1)) * 32 + 16 * (lane & 1);
+                const int page = min(max(pid, 0), a.n_pages - 1);
+                return (((size_t)page * a.H + h) << a.log_ps) * P + (size_t)((t & ps_mask) * P);
+            };
+            int next_ids = page_ids(0);
+            size_t bases = 0;
+            struct Codes {
+                uint32_t k[KW], v[2][NSV][2];
+            } ring[NB];
+            auto fetch = [&](int step, Codes &c) {
+                if ((step & 31) == 0) {
+                    bases = block_base(step, next_ids);
+                    next_ids = page_ids(step + 32);
+                }
+                size_t base[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int from = 2 * (step & 31) + k;
+                    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bases, from);
+                    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(bases >> 32), from);
+                    base[k] = ((size_t)hi << 32) | lo;
+                }
+                const uint8_t *kp = a.k_codes + (ln < 16 ? base[0] : base[1]) + k_off;
+                constexpr int BYTES = KW >= 4 ? 16 : KW * 4;
+#pragma unroll
+                for (int n = 0; n < KW; n += BYTES / 4) {
+                    const typename Raw<BYTES>::type u = global_read<BYTES>(kp + 4 * n);
+                    __builtin_memcpy(&c.k[n], &u, BYTES);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int n = 0; n < NSV; ++n) {
+                        const Raw<8>::type u = global_read<8>(a.v_codes + base[k] + v_off + 16 * n);
+                        c.v[k][n][0] = u.x;
+                        c.v[k][n][1] = u.y;
+                    }
+            };
+#pragma unroll
+            for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
+
+            auto body = [&](int step, Codes &codes) {
+                const int t0 = tile_at(step) * 32;
+                // scores
+                float16_t s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    V16 op;
+#pragma unroll
+                    for (int n = 0; n < CPS; ++n) {
+                        const int at = c * CPS + n;
+                        const uint32_t word = codes.k[at / 4];
+                        unsigned addr;
+                        if constexpr (COPIES) {
+                            addr = (at & 3) == 0 ? row_address<0>(word, k_const) : (at & 3) == 1 ? row_address<1>(word, k_const)
+                                   : (at & 3) == 2 ? row_address<2>(word, k_const) : row_address<3>(word, k_const);
+                        } else {
+                            addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
+                        }
+                        lds_read<ES>(addr, &op.w[n * (ES / 4)]);
+                    }
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(op.h8, qf[c], s, 0, 0, 0);
+                }
+                if constexpr (MODS) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float z = a.cap_out > 0.f ? a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f) : s[e] * a.scale2;
+                        const int key = t0 + 16 * (e >> 3) + 8 * lh + (e & 7);
+                        s[e] = z - slope2 * fabsf((float)(pos - key));
+                    }
+                }
+                if (!((t0 + 31 <= pos_f && t0 + 31 < r.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= r.prefix)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int key = t0 + 16 * (e >> 3) + 8 * lh + (e & 7);
+                        const bool see = (key <= see_to && key >= see_from) || key < r.prefix;
+                        s[e] = see ? s[e] : -INFINITY;
+                    }
+                }
+                // running maximum
+                float mt = s[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+                {
+                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+                    mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                }
+                if (!MODS) mt *= a.scale2;
+                if (__ballot(mt > m_ref + kRise)) {
+                    const float m_new = fmaxf(m_ref, mt), f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                    m_ref = m_new;
+                    lsum *= f;
+#pragma unroll
+                    for (int k = 0; k < CH; ++k)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[k][e] *= f;
+                }
+                const float sub = kHeadroom - m_ref;
+                const bool tail = t0 + 32 > r.len;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    V16 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(MODS ? s[8 * k + e] + sub : __builtin_fmaf(s[8 * k + e], a.scale2, sub));
+                        const float p1 = __builtin_amdgcn_exp2f(MODS ? s[8 * k + e + 1] + sub : __builtin_fmaf(s[8 * k + e + 1], a.scale2, sub));
+                        lsum += p0;
+                        lsum += p1;
+                        const half2_t p2 = {(half_t)p0, (half_t)p1};
+                        pf.h2[e / 2] = p2;
+                    }
+                    uint32_t g[8][CH / 2];   // channel pairs of the lane's eight keys
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int n = 0; n < NSV; ++n) {
+                            const uint32_t word = codes.v[k][n][e / 4];
+                            const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
+                                                  : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
+                            lds_read<VR>(addr + (unsigned)(n * VR), &g[e][n * (VR / 4)]);
+                        }
+                    if (tail) {   // what lies behind the request's end may be anything: zero times it has to be zero
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+#pragma unroll
+                            for (int c = 0; c < CH / 2; ++c) g[e][c] = t0 + 16 * k + 8 * lh + e < r.len ? g[e][c] : 0u;
+                    }
+#pragma unroll
+                    for (int c = 0; c < CH / 2; ++c) {
+                        V16 lo, hi;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            lo.w[e] = __builtin_amdgcn_perm(g[2 * e + 1][c], g[2 * e][c], 0x05040100u);
+                            hi.w[e] = __builtin_amdgcn_perm(g[2 * e + 1][c], g[2 * e][c], 0x07060302u);
+                        }
+                        o[2 * c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo.h8, pf.h8, o[2 * c], 0, 0, 0);
+                        o[2 * c + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi.h8, pf.h8, o[2 * c + 1], 0, 0, 0);
+                    }
+                }
+                fetch(step + NB, codes);
+            };
+            for (int st = 0; st < steps; st += NB)
+#pragma unroll
+                for (int u = 0; u < NB; ++u)
+                    if (st + u < steps) body(st + u, ring[u]);
+        }
+        {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+            lsum = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+        }
+
+        // join the wavefronts that share rows, in order of kw; group g of eight accumulators ends with wavefront g % ways
+        const bool whole = r0 == 0 && r1 == rounds;
+        float L = lsum, M = m_ref;
+        if (ways > 1) {
+            if (lh == 0) {
+                xm[wave * 32 + ln] = m_ref;
+                xl[wave * 32 + ln] = lsum;
+            }
+            __syncthreads();
+            const int w0 = wave - kw;
+            for (int k = 0; k < ways; ++k) M = fmaxf(M, xm[(w0 + k) * 32 + ln]);
+            L = 0.f;
+            for (int k = 0; k < ways; ++k) L += xl[(w0 + k) * 32 + ln] * __builtin_amdgcn_exp2f(xm[(w0 + k) * 32 + ln] - M);
+            const float f = __builtin_amdgcn_exp2f(m_ref - M);
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[k][e] *= f;
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const size_t part = part_of(a, h, w, r0 > 0 ? 0 : 1);
+        const int prow = rt * 32 + ln;
+        if (!whole && valid && lh == 0 && kw == 0) {
+            float *st = part_stats<D>(a, part) + prow * 2;
+            st[0] = M;
+            st[1] = L;
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int reg = CH == 4 ? 4 * (g >> 1) + 2 * (g & 1) + e / 4 : 4 * g + e / 2;
+                x[e] = o[e % CH][reg];
+            }
+            const bool owner = (g & (ways - 1)) == kw;
+            if (ways > 1) {
+                float4_t *mine = reinterpret_cast<float4_t *>(xs) + wave * 128;
+                if (!owner) {
+                    mine[lane] = float4_t{x[0], x[1], x[2], x[3]};
+                    mine[64 + lane] = float4_t{x[4], x[5], x[6], x[7]};
+                }
+                __syncthreads();
+                if (owner) {
+                    float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int k = 0; k < ways; ++k) {
+                        if (k == kw) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) t[e] += x[e];
+                            continue;
+                        }
+                        const float4_t *from = reinterpret_cast<const float4_t *>(xs) + (wave - kw + k) * 128;
+                        const float4_t y0 = from[lane], y1 = from[64 + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            t[e] += y0[e];
+                            t[4 + e] += y1[e];
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = t[e];
+                }
+                __syncthreads();
+            }
+            if (owner && valid) {
+                const int ch = CH == 4 ? 32 * (g >> 1) + 16 * lh + 8 * (g & 1) : 16 * g + 8 * lh;
+                if (whole) {
+                    half8_t y;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = (half_t)(x[e] * inv);
+                    *reinterpret_cast<half8_t *>(a.out + (size_t)(r.first + i) * a.out_stride + (size_t)hq * D + ch) = y;
+                } else {
+                    float4_t *to = reinterpret_cast<float4_t *>(part_sums<D>(a, part) + (size_t)prow * D + ch);
+                    to[0] = float4_t{x[0], x[1], x[2], x[3]};
+                    to[1] = float4_t{x[4], x[5], x[6], x[7]};
+                }
+            }
+        }
+    };
+
+    long long left = sh.u1 - sh.u0, x = sh.x;
+    int b = sh.b;
+    Request r = request_of(a, b);
+    while (true) {
+        const int k = (int)(x / r.C), from = (int)(x - (long long)k * r.C), take = (int)min((long long)(r.C - from), left), to = from + take;
+        const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
+        for (int piece = 0; piece < 2; ++piece) {
+            const int j = piece == 0 ? jl : k;
+            if (piece == 1 && j == jl) break;
+            const int off = piece == 0 ? 0 : nl, rounds = piece == 0 ? nl : block_rounds(a, r, k);
+            int r0 = max(from - off, 0), r1 = to == r.C ? rounds : min(to - off, rounds);
+            if (!a.cut) {   // whole blocks, with the share that they begin in
+                const bool mine = off >= from && (off < to || to == r.C);
+                r0 = 0;
+                r1 = mine ? rounds : 0;
+            }
+            if (r0 < r1) run_block(r, b, j, r0, r1, rounds);
+        }
+        left -= take;
+        x += take;
+        if (left <= 0) break;
+        if (x == (long long)r.items * r.C) {
+            x = 0;
+            do r = request_of(a, ++b);   // (requests without new tokens have no rounds; the share's end lies before the last request's)
+            while (r.blocks == 0);
+        }
+    }
+}
+
+// Joins the sums of the block that worker w's share begins inside, if no worker before it began there too.
+template <int D>
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedArgs a) {
+    __shared__ long long xs[256 / 64 + 2];
+    const int w = blockIdx.x + 1, h = blockIdx.y, tid = threadIdx.x;
+    Share sh;
+    if (!find_share<256>(a, w, xs, &sh)) return;
+    const Request r = request_of(a, sh.b);
+    const int k = (int)(sh.x / r.C), from = (int)(sh.x - (long long)k * r.C);
+    const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
+    int j = jl, off = 0, rounds = nl;
+    if (from >= nl) {
+        if (k == jl) return;
+        j = k;
+        off = nl;
+        rounds = block_rounds(a, r, k);
+    }
+    if (from <= off || from >= off + rounds || from - sh.share > off) return;
+    // pieces: the end of worker w - 1's share, then the beginnings of w's and of those behind it that begin inside the block
+    const long long end = sh.u0 - from + min(off + rounds, r.C);
+    const int pieces = 1 + (int)((end - sh.u0 + sh.share - 1) / sh.share);
+    const int row0 = j * block_rows(r), rows = min(block_rows(r), r.rows - row0);
+    constexpr int PER = D / 8;   // threads of a row
+    for (int t = tid; t < rows * PER; t += 256) {
+        const int lr = t / PER, ch = (t - lr * PER) * 8, row = row0 + lr;
+        float M = -FLT_MAX, L = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        auto part = [&](int p) { return part_of(a, h, w - 1 + p, p == 0 ? 1 : 0); };
+        for (int p = 0; p < pieces; ++p) M = fmaxf(M, part_stats<D>(a, part(p))[lr * 2]);
+        for (int p = 0; p < pieces; ++p) {
+            const float *st = part_stats<D>(a, part(p)) + lr * 2;
+            const float f = __builtin_amdgcn_exp2f(st[0] - M);
+            L += st[1] * f;
+            const float4_t *y = reinterpret_cast<const float4_t *>(part_sums<D>(a, part(p)) + (size_t)lr * D + ch);
+            const float4_t y0 = y[0], y1 = y[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] += y0[e] * f;
+                x[4 + e] += y1[e] * f;
+            }
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        half8_t y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (half_t)(x[e] * inv);
+        const int i = row / a.group, hq = h * a.group + (row - i * a.group);
+        *reinterpret_cast<half8_t *>(a.out + (size_t)(r.first + i) * a.out_stride + (size_t)hq * D + ch) = y;
+    }
+}
+
+// How a call is cut, from its sizes alone.
+struct PagedPlan {
+    int workers, min_log_ways, cut;
+    size_t ws;
+};
+PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
+    PagedPlan p;
+    p.workers = kv->H >= 256 ? 1 : 256 / kv->H;
+    const long long rows = (long long)b->n_tokens * (b->Hq / kv->H) * kv->H;
+    p.min_log_ways = rows >= 256 * 1024 ? 0 : rows >= 128 * 1024 ? 1 : 2;
+    p.cut = p.workers > 1 && (long long)b->max_pages * kv->page_tokens > 512;
+    p.ws = p.cut ? (size_t)kv->H * p.workers * 2 * ((kWaves * 32) >> p.min_log_ways) * (kv->D + 2) * sizeof(float) : 0;
+    return p;
+}
+
+template <int D, int V, bool COPIES, bool MODS>
+int run_paged(const PagedArgs &a, hipStream_t s) {
+    static KernelSetup setup;
+    if (int st = kernel_setup(reinterpret_cast<const void *>(&attn_paged_kernel<D, V, COPIES, MODS>), kLds, true, setup)) return st;
+    attn_paged_kernel<D, V, COPIES, MODS><<<a.H * a.workers, kThreads, kLds, s>>>(a);
+    if (a.cut) attn_paged_merge_kernel<D><<<dim3(a.workers - 1, a.H), 256, 0, s>>>(a);
+    return launch_status();
+}
+template <int D, int V>
+int run_paged_as(const PagedArgs &a, hipStream_t s) {
+    const bool mods = a.cap_out > 0.f || a.slopes;
+    if (a.G == 1) return mods ? run_paged<D, V, true, true>(a, s) : run_paged<D, V, true, false>(a, s);
+    return mods ? run_paged<D, V, false, true>(a, s) : run_paged<D, V, false, false>(a, s);
 }
 
 }  // namespace
@@ -77,10 +708,11 @@ bool attn_paged_supported(const vq_kv_pages_t *kv) {
     return (kv->D == 64 || kv->D == 128) && (PG & (PG - 1)) == 0;
 }
 
-size_t attn_paged_workspace(const vq_kv_pages_t *, const vq_paged_batch_t *) { return 0; }
+size_t attn_paged_workspace(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) { return paged_plan(kv, b).ws; }
 
 int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const void *q, size_t q_stride, float sm_scale, void *out,
-                      size_t out_stride, void *, hipStream_t s) {
+                      size_t out_stride, void *ws, hipStream_t s) {
+    const PagedPlan p = paged_plan(kv, b);
     PagedArgs a;
     a.k_codes = (const uint8_t *)kv->k_codes;
     a.v_codes = (const uint8_t *)kv->v_codes;
@@ -93,6 +725,7 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.slopes = b->slopes;
     a.q = (const half_t *)q;
     a.out = (half_t *)out;
+    a.ws = (float *)ws;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.B = b->B;
@@ -100,17 +733,23 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.group = b->Hq / kv->H;
     a.E = kv->n_entries;
     a.G = kv->cb_groups;
+    a.pg_shift = __builtin_ctz(kv->D / kv->v / kv->cb_groups);
     a.n_pages = kv->n_pages;
     a.max_pages = b->max_pages;
     a.log_ps = __builtin_ctz(kv->page_tokens);
     a.n_tokens = b->n_tokens;
-    a.window = b->window;
-    a.scale = sm_scale;
-    a.softcap = b->softcap;
-    const dim3 grid(b->n_tokens, b->Hq);
-    if (kv->D == 64) attn_paged_row_kernel<64><<<grid, 64, 0, s>>>(a, kv->v);
-    else attn_paged_row_kernel<128><<<grid, 64, 0, s>>>(a, kv->v);
-    return launch_status();
+    a.window = b->window < b->max_pages * kv->page_tokens ? b->window : 0;   // (one that reaches every token is none)
+    a.workers = p.workers;
+    a.min_log_ways = p.min_log_ways;
+    a.cut = p.cut;
+    a.min_share = 2;
+    const float scale = sm_scale < 0.f ? -sm_scale : sm_scale;
+    a.scale2 = scale * kLog2e > FLT_MIN ? scale * kLog2e : FLT_MIN;   // (above zero: minus infinity times it has to stay)
+    a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;
+    a.cap_out = b->softcap * kLog2e;
+    a.cap_in = b->softcap > 0.f ? 2.f * a.scale2 / b->softcap : 0.f;
+    if (kv->D == 64) return kv->v == 8 ? run_paged_as<64, 8>(a, s) : kv->v == 4 ? run_paged_as<64, 4>(a, s) : run_paged_as<64, 2>(a, s);
+    return kv->v == 8 ? run_paged_as<128, 8>(a, s) : kv->v == 4 ? run_paged_as<128, 4>(a, s) : run_paged_as<128, 2>(a, s);
 }
 
 }  // namespace vq
