@@ -401,15 +401,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
             for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
 
-            auto body = [&](int step, Codes &codes) {
-                const int t0 = tile_at(step) * 32;
-                // scores
-                float16_t s;
+            // K entries of the next tile as operands (each tile's gathers are requested a tile ahead)
+            V16 kop[NC];
+            auto gather_k = [&](const Codes &codes) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    V16 op;
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int n = 0; n < CPS; ++n) {
                         const int at = c * CPS + n;
@@ -421,10 +417,54 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         } else {
                             addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
                         }
-                        lds_read<ES>(addr, &op.w[n * (ES / 4)]);
+                        lds_read<ES>(addr, &kop[c].w[n * (ES / 4)]);
                     }
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(op.h8, qf[c], s, 0, 0, 0);
+            };
+            gather_k(ring[0]);
+
+            auto body = [&](int step, Codes &codes, const Codes &next) {
+                const int t0 = tile_at(step) * 32;
+                if (t0 + 32 > r.len) {
+                    // Codes behind the request's end may name anything, and a weight of zero times an infinity is none: they become the
+                    // tile's first token's (a lane's run of eight keys ends at its first one, or does not begin).
+#pragma unroll
+                    for (int n = 0; n < NSV; ++n) {
+                        const unsigned own = codes.v[0][n][0] & 0xFFu;
+                        const auto x = __builtin_amdgcn_permlane32_swap(own, own, false, false);
+                        const uint32_t good = x[0] * 0x01010101u;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int d = 0; d < 2; ++d) {
+                                const int live = min(max(r.len - (t0 + 16 * k + 8 * lh + 4 * d), 0), 4);   // bytes that stay
+                                const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << (8 * live)) - 1u;
+                                codes.v[k][n][d] = (codes.v[k][n][d] & mask) | (good & ~mask);
+                            }
+                    }
                 }
+                uint32_t g[2][8][CH / 2];   // channel pairs of the lane's eight keys of a block
+                auto gather_v = [&](int k) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int n = 0; n < NSV; ++n) {
+                            const uint32_t word = codes.v[k][n][e / 4];
+                            const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
+                                                  : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
+                            lds_read<VR>(addr + (unsigned)(n * VR), &g[k][e][n * (VR / 4)]);
+                        }
+                };
+                __builtin_amdgcn_sched_barrier(0);
+                // scores; the first values' gathers run beside them, the next tile's keys' behind them
+                float16_t s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kop[c].h8, qf[c], s, 0, 0, 0);
+                gather_v(0);
+                __builtin_amdgcn_sched_barrier(0);
+                gather_k(next);
+                __builtin_amdgcn_sched_barrier(0);
                 if constexpr (MODS) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -460,7 +500,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         for (int e = 0; e < 16; ++e) o[k][e] *= f;
                 }
                 const float sub = kHeadroom - m_ref;
-                const bool tail = t0 + 32 > r.len;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     V16 pf;
@@ -473,40 +512,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         const half2_t p2 = {(half_t)p0, (half_t)p1};
                         pf.h2[e / 2] = p2;
                     }
-                    uint32_t g[8][CH / 2];   // channel pairs of the lane's eight keys
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int n = 0; n < NSV; ++n) {
-                            const uint32_t word = codes.v[k][n][e / 4];
-                            const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
-                                                  : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
-                            lds_read<VR>(addr + (unsigned)(n * VR), &g[e][n * (VR / 4)]);
-                        }
-                    if (tail) {   // what lies behind the request's end may be anything: zero times it has to be zero
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-#pragma unroll
-                            for (int c = 0; c < CH / 2; ++c) g[e][c] = t0 + 16 * k + 8 * lh + e < r.len ? g[e][c] : 0u;
-                    }
 #pragma unroll
                     for (int c = 0; c < CH / 2; ++c) {
                         V16 lo, hi;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            lo.w[e] = __builtin_amdgcn_perm(g[2 * e + 1][c], g[2 * e][c], 0x05040100u);
-                            hi.w[e] = __builtin_amdgcn_perm(g[2 * e + 1][c], g[2 * e][c], 0x07060302u);
+                            lo.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][c], g[k][2 * e][c], 0x05040100u);
+                            hi.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][c], g[k][2 * e][c], 0x07060302u);
                         }
                         o[2 * c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo.h8, pf.h8, o[2 * c], 0, 0, 0);
                         o[2 * c + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi.h8, pf.h8, o[2 * c + 1], 0, 0, 0);
                     }
+                    if (k == 0) gather_v(1);
                 }
                 fetch(step + NB, codes);
             };
             for (int st = 0; st < steps; st += NB)
 #pragma unroll
                 for (int u = 0; u < NB; ++u)
-                    if (st + u < steps) body(st + u, ring[u]);
+                    if (st + u < steps) body(st + u, ring[u], ring[(u + 1) % NB]);
         }
         {
             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
