@@ -96,7 +96,7 @@ static int check_page_step(const vq_page_step_t *p) {
 static int check_paged_sizes(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     if (int st = check_kv_pages(kv)) return st;
     if (!b) return VQ_ERR_NULL;
-    if (kv->H < 1 || b->B < 0 || b->B > kMostRequests || b->max_pages < 1 || (long long)b->B * b->max_pages > INT_MAX ||
+    if (kv->H < 1 || kv->n_pages < 1 || b->B < 0 || b->B > kMostRequests || b->max_pages < 1 || (long long)b->B * b->max_pages > INT_MAX ||
         (long long)b->max_pages * kv->page_tokens > kMostLength || b->n_tokens < 0 || b->n_tokens > kMostTokens || b->Hq < 1 || b->Hq % kv->H != 0 ||
         (long long)b->n_tokens * (b->Hq / kv->H) > INT_MAX || b->window < 0 || !(b->softcap >= 0.f) || b->softcap > FLT_MAX)
         return VQ_ERR_SHAPE;

@@ -24,6 +24,7 @@
 // with one scan over the requests.  A block cut by a share's border leaves its sums in ws, and attn_paged_merge_kernel joins them in order.
 #include <cfloat>
 #include <climits>
+#include <type_traits>
 
 #include "vq_common.h"
 
@@ -37,7 +38,8 @@ constexpr int kSide = 65536;                  // LDS of a side's codebooks
 constexpr int kJoinOff = 2 * kSide;           // sums of wavefronts that share rows, 2 KiB each
 constexpr int kStatOff = kJoinOff + 16384;    // their maxima and sums of weights, [wave][32] each
 constexpr int kScanOff = kStatOff + 2048;
-constexpr int kLds = kScanOff + 256;
+constexpr int kListOff = kScanOff + 256;      // pieces of the share, 64 at a time: their first rounds, and a Piece each
+constexpr int kLds = kListOff + 256 + 64 * 64;
 constexpr float kHeadroom = 6.f, kRise = 8.f; // (log2)
 
 struct PagedArgs {
@@ -50,6 +52,8 @@ struct PagedArgs {
     float *ws;
     size_t q_stride, out_stride;
     int B, H, group, E, G, pg_shift, n_pages, max_pages, log_ps, n_tokens, window;
+    unsigned group_inverse;   // row / group = row * group_inverse >> group_shift, for rows below 2^31
+    int group_shift;
     int workers;        // workgroups of a cache head
     int min_log_ways;   // fewest wavefronts that share 32 rows
     int cut;            // 0: blocks are not cut
@@ -58,6 +62,8 @@ struct PagedArgs {
     unsigned q_sign;    // sign of sm_scale, in both halves
     float cap_in, cap_out;   // softcap: cap_out - 2 cap_out / (2^(s cap_in) + 1), 0: none
 };
+
+__device__ __forceinline__ int token_of(const PagedArgs &a, int row) { return (int)(((unsigned long long)(unsigned)row * a.group_inverse) >> a.group_shift); }
 
 // A request, in numbers that fit no memory access out of bounds.
 struct Request {
@@ -79,7 +85,7 @@ __device__ __forceinline__ Tiles tiles_of(const PagedArgs &a, const Request &r, 
 __device__ __forceinline__ int block_rows(const Request &r) { return (kWaves * 32) >> r.log_ways; }
 __device__ __forceinline__ Tiles block_tiles(const PagedArgs &a, const Request &r, int j) {
     const int row = j * block_rows(r);
-    return tiles_of(a, r, row / a.group, (min(row + block_rows(r), r.rows) - 1) / a.group);
+    return tiles_of(a, r, token_of(a, row), token_of(a, min(row + block_rows(r), r.rows) - 1));
 }
 __device__ __forceinline__ int block_rounds(const PagedArgs &a, const Request &r, int j) {   // (a block that attends nothing writes zeros)
     return max((block_tiles(a, r, j).count() + (1 << r.log_ways) - 1) >> r.log_ways, 1);
@@ -89,7 +95,7 @@ __device__ __forceinline__ Request request_of(const PagedArgs &a, int b) {
     const int c0 = min(max(a.cu_new[b], 0), a.n_tokens), c1 = min(max(a.cu_new[b + 1], 0), a.n_tokens);
     r.first = c0;
     r.n = max(c1 - c0, 0);
-    r.len = a.n_pages > 0 ? min(max(a.seq_lens[b], 0), a.max_pages << a.log_ps) : 0;
+    r.len = min(max(a.seq_lens[b], 0), a.max_pages << a.log_ps);
     r.prefix = a.prefix_lens ? min(max(a.prefix_lens[b], 0), r.len) : 0;
     r.rows = r.n * a.group;
     r.log_ways = max(r.rows <= 32 ? 3 : r.rows <= 64 ? 2 : r.rows <= 128 ? 1 : 0, a.min_log_ways);
@@ -179,6 +185,125 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, int w, long long 
     return true;
 }
 
+// Rounds [r0, r1) of a block of a request.
+struct alignas(16) Piece {
+    int first, pos0, len, prefix;       // of the request: its first row of q, length before its new tokens, length, prefix
+    int rows, log_ways, row0, b;        // rows of the request, first row of the block
+    int front, lo, count, whole;        // tiles of the block: [0, front) and [lo, ...), count in all; r0 .. r1 is all of it
+    int r0, r1, pad0, pad1;
+};
+__device__ __forceinline__ Piece uniform_piece(const Piece &p) {
+    Piece u;
+    constexpr int N = sizeof(Piece) / 4;
+    int t[N];
+    __builtin_memcpy(t, &p, sizeof(Piece));
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_readfirstlane(t[i]);
+    __builtin_memcpy(&u, t, sizeof(Piece));
+    return u;
+}
+__device__ __forceinline__ long long shfl_ll(long long v, int from) {
+    return ((long long)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, from);
+}
+
+// The next pieces of a share, 64 at most: from round *x of request *b on, *left rounds; all three step behind them.  A lane makes a piece:
+// of one request (as many as have a single block), or of one block of a larger request.  Every wavefront of the workgroup makes the same list,
+// one writes it.  Returns the pieces; *rounds: theirs, each piece's rounded up to PAD.
+template <int PAD>
+__device__ __forceinline__ int list_pieces(const PagedArgs &a, int *b, long long *x, long long *left, bool write, int *starts, Piece *list, int *rounds) {
+    static_assert((PAD & (PAD - 1)) == 0, "");
+    const int lane = threadIdx.x & 63;
+    Request r = {};
+    if (*b + lane < a.B) r = request_of(a, *b + lane);
+    Piece pc = {};
+    int from, to, j = 0, off = 0, n = 0;   // rounds [from, to) of the item; the block's first in it, the block's number of them
+    bool there;
+    const unsigned long long large = __ballot(r.blocks > 1);
+    if (large & 1) {
+        Request u;
+        constexpr int N = sizeof(Request) / 4;
+        int t[N];
+        __builtin_memcpy(t, &r, sizeof(Request));
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_readfirstlane(t[i]);
+        __builtin_memcpy(&u, t, sizeof(Request));
+        r = u;
+        const int k0 = (int)(*x / r.C), from0 = (int)(*x - (long long)k0 * r.C), ahead = lane >> 1, k = k0 + ahead;
+        const long long before = ahead == 0 ? 0 : (long long)ahead * r.C - from0;
+        from = ahead == 0 ? from0 : 0;
+        to = from + (int)min(max(*left - before, 0ll), (long long)(r.C - from));
+        there = k < r.items && to > from;
+        if (there) {
+            const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
+            j = (lane & 1) ? k : jl;
+            off = (lane & 1) ? nl : 0;
+            n = (lane & 1) ? block_rounds(a, r, k) : nl;
+            there = !((lane & 1) && k == jl);
+        }
+        const long long taken = min(*left, (long long)(min(k0 + 32, r.items) - k0) * r.C - from0);
+        *left -= taken;
+        *x += taken;
+        pc.b = *b;
+        if (*x == (long long)r.items * r.C) {
+            *x = 0;
+            *b += 1;
+        }
+    } else {
+        const int simple = large ? __ffsll((long long)large) - 1 : 64;
+        from = lane == 0 ? (int)*x : 0;
+        const int avail = lane < simple ? r.items * r.C - from : 0;
+        long long upto = avail;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long y = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += y;
+        }
+        to = from + (int)min(max(*left - (upto - avail), 0ll), (long long)avail);
+        there = to > from;
+        n = there ? block_rounds(a, r, 0) : 0;
+        *left -= min(*left, shfl_ll(upto, 63));
+        pc.b = *b + lane;
+        *x = 0;
+        *b += simple;
+    }
+    if (a.cut) {
+        pc.r0 = max(from - off, 0);
+        pc.r1 = to == r.C ? n : min(to - off, n);
+    } else {   // whole blocks, with the share that they begin in
+        pc.r0 = 0;
+        pc.r1 = off >= from && (off < to || to == r.C) ? n : 0;
+    }
+    there = there && pc.r0 < pc.r1;
+    pc.whole = pc.r0 == 0 && pc.r1 == n;
+    const int mine = there ? (pc.r1 - pc.r0 + PAD - 1) & -PAD : 0;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += y;
+    }
+    *rounds = __builtin_amdgcn_readlane(upto, 63);
+    const unsigned long long all = __ballot(there);
+    if (write && there) {
+        const Tiles t = block_tiles(a, r, j);
+        pc.first = r.first;
+        pc.pos0 = r.len - r.n;
+        pc.len = r.len;
+        pc.prefix = r.prefix;
+        pc.rows = r.rows;
+        pc.log_ways = r.log_ways;
+        pc.row0 = j * block_rows(r);
+        pc.front = t.front;
+        pc.lo = t.lo;
+        pc.count = t.count();
+        pc.pad0 = pc.pad1 = 0;
+        const int at = __popcll(all & ((1ull << lane) - 1ull));
+        starts[at] = upto - mine;
+        list[at] = pc;
+    }
+    return __popcll(all);
+}
+
 // Sums of cut blocks: two per worker (the block that its share begins inside, the one that it ends inside), [rows][D] and [rows][2].
 __device__ __forceinline__ size_t part_of(const PagedArgs &a, int h, int w, int which) { return ((size_t)h * a.workers + w) * 2 + which; }
 __device__ __forceinline__ int part_rows(const PagedArgs &a) { return (kWaves * 32) >> a.min_log_ways; }
@@ -230,13 +355,13 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = (tid + i * kThreads) >> 4;
-            e[i] = row < a.E ? global_read<ES>(kc + (size_t)row * ES) : none;
+            e[i] = global_read<ES>(kc + (unsigned)(min(row, a.E - 1) * ES));
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             entry_t r[16 / ES];
 #pragma unroll
-            for (int k = 0; k < 16 / ES; ++k) r[k] = e[i];
+            for (int k = 0; k < 16 / ES; ++k) r[k] = ((tid + i * kThreads) >> 4) < a.E ? e[i] : none;
             uint4 u;
             __builtin_memcpy(&u, r, 16);
             reinterpret_cast<uint4 *>(smem)[tid + i * kThreads] = u;
@@ -247,10 +372,10 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = tid + i * kThreads, row = u & 255, p = u >> 8;
-            e[i] = row < a.E ? global_read<ES>(kc + ((size_t)(p >> a.pg_shift) * a.E + row) * ES) : none;
+            e[i] = global_read<ES>(kc + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES));
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(smem)[tid + i * kThreads] = e[i];
+        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(smem)[tid + i * kThreads] = ((tid + i * kThreads) & 255) < a.E ? e[i] : none;
     }
     constexpr int CH = D / 32, US = 2 * (V < CH ? V : CH), UNITS = 2 * D / US;   // parts of an entry that one lane takes
     constexpr int N = 256 * UNITS / kThreads;
@@ -272,13 +397,13 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
         int row, unit;
         place(i, &row, &unit);
         const int ch = unit * (US / 2), p = ch / V;
-        e[i] = row < a.E ? global_read<US>(vc + ((size_t)(p >> a.pg_shift) * a.E + row) * ES + (ch % V) * 2) : zero;
+        e[i] = global_read<US>(vc + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES + (ch % V) * 2));
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         int row, unit;
         place(i, &row, &unit);
-        *reinterpret_cast<unit_t *>(smem + kSide + row * 256 + unit * US) = e[i];
+        *reinterpret_cast<unit_t *>(smem + kSide + row * 256 + unit * US) = row < a.E ? e[i] : zero;
     }
 }
 
@@ -302,8 +427,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
     Share sh;
     if (!find_share<kThreads>(a, w, reinterpret_cast<long long *>(smem + kScanOff), &sh)) return;
-    stage_tables<D, V, COPIES>(a, h, smem, tid);
-    __syncthreads();
 
     const int ps_mask = (1 << a.log_ps) - 1;
     // lane constants of the gathers
@@ -313,32 +436,109 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int key16 = 8 * ((ln >> 2) & 1) + 4 * ((ln >> 3) & 1) + (ln & 3);
     const unsigned k_off = (unsigned)(key16 * P + lh * (P / 2)), v_off = (unsigned)(ln * CH / V * 16 + lh * 8);
     float *xs = reinterpret_cast<float *>(smem + kJoinOff), *xm = reinterpret_cast<float *>(smem + kStatOff), *xl = xm + kWaves * 32;
+    int *starts = reinterpret_cast<int *>(smem + kListOff);
+    Piece *list = reinterpret_cast<Piece *>(smem + kListOff + 256);
 
-    // rounds [r0, r1) of block j of request r
-    auto run_block = [&](const Request &r, int b, int j, int r0, int r1, int rounds) {
-        const int ways = 1 << r.log_ways, rt = wave >> r.log_ways, kw = wave & (ways - 1);
-        const int row0 = j * block_rows(r) + rt * 32, tile_rows = min(r.rows - row0, 32);
-        const Tiles bt = block_tiles(a, r, j);
-        const bool valid = ln < tile_rows;
-        const int row = valid ? row0 + ln : min(row0, r.rows - 1), i = row / a.group, hq = h * a.group + (row - i * a.group);
-        const int pos = r.len - r.n + i;
+    long long left = sh.u1 - sh.u0, x = sh.x;
+    int b = sh.b;
+    bool staged = false;
+    while (left > 0) {
+        int rounds_in_list;
+        __syncthreads();   // (the list before is done with)
+        const int pieces = list_pieces<NB>(a, &b, &x, &left, wave == 0, starts, list, &rounds_in_list);
+        __syncthreads();
+        if (pieces == 0) continue;
 
-        float16_t o[CH];
+        // Pages of 32 rounds of this wavefront at a time: lane 2 s + k finds the first byte of the codes of block k (16 tokens) of
+        // round s.  The list is one sequence of rounds, so codes are requested across its pieces' borders.
+        int next_id, next_off;
+        auto page_ids = [&](int step) {
+            const int t = min(step + (lane >> 1), rounds_in_list - 1);
+            int p = 0;
 #pragma unroll
-        for (int f = 0; f < CH; ++f)
+            for (int d = 32; d; d >>= 1)
+                if (p + d < pieces && starts[p + d] <= t) p += d;
+            const Piece &pc = list[p];
+            const int idx = max(min(((pc.r0 + t - starts[p]) << pc.log_ways) + (wave & ((1 << pc.log_ways) - 1)), pc.count - 1), 0);
+            const int at = (idx < pc.front ? idx : pc.lo + idx - pc.front) * 32 + 16 * (lane & 1);
+            next_id = a.table[(size_t)pc.b * a.max_pages + (max(min(at, pc.len - 1), 0) >> a.log_ps)];
+            next_off = (at & ps_mask) * P;
+        };
+        page_ids(0);
+        size_t bases = 0;
+        struct Codes {
+            uint32_t k[KW], v[2][NSV][2];
+        } ring[NB];
+        auto fetch = [&](int step, Codes &c) {
+            if ((step & 31) == 0) {
+                bases = (((size_t)min(max(next_id, 0), a.n_pages - 1) * a.H + h) << a.log_ps) * P + (size_t)next_off;
+                page_ids(step + 32);
+            }
+            size_t base[2];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
-        float m_ref = -FLT_MAX, lsum = 0.f;
+            for (int k = 0; k < 2; ++k) {
+                const int from = 2 * (step & 31) + k;
+                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bases, from);
+                const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(bases >> 32), from);
+                base[k] = ((size_t)hi << 32) | lo;
+            }
+            const uint8_t *kp = a.k_codes + (ln < 16 ? base[0] : base[1]) + k_off;
+            constexpr int BYTES = KW >= 4 ? 16 : KW * 4;
+#pragma unroll
+            for (int n = 0; n < KW; n += BYTES / 4) {
+                const typename Raw<BYTES>::type u = global_read<BYTES>(kp + 4 * n);
+                __builtin_memcpy(&c.k[n], &u, BYTES);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < NSV; ++n) {
+                    const Raw<8>::type u = global_read<8>(a.v_codes + base[k] + v_off + 16 * n);
+                    c.v[k][n][0] = u.x;
+                    c.v[k][n][1] = u.y;
+                }
+        };
+#pragma unroll
+        for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
+        if (!staged) {   // (while the first codes are on their way)
+            int t = tid;
+            asm volatile("" : "+v"(t));   // (or its addresses are formed before the loop, and lie in scratch)
+            stage_tables<D, V, COPIES>(a, h, smem, t);
+            __syncthreads();
+            staged = true;
+        }
+        // K entries of the next tile as operands (each tile's gathers are requested a tile ahead)
+        V16 kop[NC];
+        auto gather_k = [&](const Codes &codes) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int n = 0; n < CPS; ++n) {
+                    const int at = c * CPS + n;
+                    const uint32_t word = codes.k[at / 4];
+                    unsigned addr;
+                    if constexpr (COPIES) {
+                        addr = (at & 3) == 0 ? row_address<0>(word, k_const) : (at & 3) == 1 ? row_address<1>(word, k_const)
+                               : (at & 3) == 2 ? row_address<2>(word, k_const) : row_address<3>(word, k_const);
+                    } else {
+                        addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
+                    }
+                    lds_read<ES>(addr, &kop[c].w[n * (ES / 4)]);
+                }
+        };
+        gather_k(ring[0]);
 
-        const int i0 = row0 / a.group, i1 = (row0 + tile_rows - 1) / a.group;
-        const int count = tile_rows > 0 ? bt.front + max(min(tiles_of(a, r, i0, i1).hi, bt.hi) - bt.lo, 0) : 0;
-        const int idx0 = r0 * ways + kw, idx_end = min(r1 * ways, count);
-        const int steps = idx0 < idx_end ? (idx_end - idx0 + ways - 1) >> r.log_ways : 0;
-        if (steps > 0) {
-            const int pos_f = r.len - r.n + i0, pos_l = r.len - r.n + i1;
+        int step = 0;
+        for (int piece = 0; piece < pieces; ++piece) {
+            const Piece pc = uniform_piece(list[piece]);
+            const int ways = 1 << pc.log_ways, rt = wave >> pc.log_ways, kw = wave & (ways - 1);
+            const int row0 = pc.row0 + rt * 32, tile_rows = min(pc.rows - row0, 32);
+            const bool valid = ln < tile_rows;
+            const int row = valid ? row0 + ln : min(row0, pc.rows - 1), i = token_of(a, row), hq = h * a.group + (row - i * a.group);
+            const int pos = pc.pos0 + i;
             half8_t qf[NC];
             {
-                const half_t *qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)hq * D + lh * (D / 2);
+                const half_t *qp = a.q + (size_t)(pc.first + i) * a.q_stride + (size_t)hq * D + lh * (D / 2);
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
                     V16 u = ld16(qp + 8 * c);
@@ -347,96 +547,39 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     qf[c] = u.h8;
                 }
             }
+            float16_t o[CH];
+#pragma unroll
+            for (int f = 0; f < CH; ++f)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
+            float m_ref = -FLT_MAX, lsum = 0.f;
+            // tiles of this wavefront's rows, of those of the block
+            const int pos_f = pc.pos0 + token_of(a, max(row0, 0)), pos_l = pc.pos0 + token_of(a, max(row0 + tile_rows - 1, 0));
+            const int count = tile_rows > 0 ? min(pc.front + max(((max(pos_l + 1, pc.prefix) + 31) >> 5) - pc.lo, 0), pc.count) : 0;
             const float slope2 = MODS && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
-            const int see_to = min(pos, r.len - 1), see_from = a.window > 0 ? pos - a.window + 1 : INT_MIN;
+            const int see_to = min(pos, pc.len - 1), see_from = a.window > 0 ? pos - a.window + 1 : INT_MIN;
 
-            auto tile_at = [&](int step) {
-                const int idx = min(idx0 + (step << r.log_ways), idx_end - 1);
-                return idx < bt.front ? idx : bt.lo + idx - bt.front;
-            };
-            // Pages of 32 steps at a time: lane 2 s + k holds the first byte of the codes of block k of step s.
-            auto page_ids = [&](int step) {
-                const int t = min(tile_at(step + (lane >> 1)) * 32 + 16 * (lane & 1), r.len - 1);
-                return a.table[(size_t)b * a.max_pages + (t >> a.log_ps)];
-            };
-            auto block_base = [&](int step, int pid) {
-                const int t = tile_at(step + (lane >> 1)) * 32 + 16 * (lane & 1);
-                const int page = min(max(pid, 0), a.n_pages - 1);
-                return (((size_t)page * a.H + h) << a.log_ps) * P + (size_t)((t & ps_mask) * P);
-            };
-            int next_ids = page_ids(0);
-            size_t bases = 0;
-            struct Codes {
-                uint32_t k[KW], v[2][NSV][2];
-            } ring[NB];
-            auto fetch = [&](int step, Codes &c) {
-                if ((step & 31) == 0) {
-                    bases = block_base(step, next_ids);
-                    next_ids = page_ids(step + 32);
+            auto body = [&](int round, Codes &codes, const Codes &next) {
+                const int idx = (round << pc.log_ways) + kw;
+                if (idx >= count || round >= pc.r1) {   // (nothing for these rows in this round)
+                    gather_k(next);
+                    fetch(step + NB, codes);
+                    return;
                 }
-                size_t base[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int from = 2 * (step & 31) + k;
-                    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bases, from);
-                    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(bases >> 32), from);
-                    base[k] = ((size_t)hi << 32) | lo;
-                }
-                const uint8_t *kp = a.k_codes + (ln < 16 ? base[0] : base[1]) + k_off;
-                constexpr int BYTES = KW >= 4 ? 16 : KW * 4;
-#pragma unroll
-                for (int n = 0; n < KW; n += BYTES / 4) {
-                    const typename Raw<BYTES>::type u = global_read<BYTES>(kp + 4 * n);
-                    __builtin_memcpy(&c.k[n], &u, BYTES);
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int n = 0; n < NSV; ++n) {
-                        const Raw<8>::type u = global_read<8>(a.v_codes + base[k] + v_off + 16 * n);
-                        c.v[k][n][0] = u.x;
-                        c.v[k][n][1] = u.y;
-                    }
-            };
-#pragma unroll
-            for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
-
-            // K entries of the next tile as operands (each tile's gathers are requested a tile ahead)
-            V16 kop[NC];
-            auto gather_k = [&](const Codes &codes) {
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int n = 0; n < CPS; ++n) {
-                        const int at = c * CPS + n;
-                        const uint32_t word = codes.k[at / 4];
-                        unsigned addr;
-                        if constexpr (COPIES) {
-                            addr = (at & 3) == 0 ? row_address<0>(word, k_const) : (at & 3) == 1 ? row_address<1>(word, k_const)
-                                   : (at & 3) == 2 ? row_address<2>(word, k_const) : row_address<3>(word, k_const);
-                        } else {
-                            addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
-                        }
-                        lds_read<ES>(addr, &kop[c].w[n * (ES / 4)]);
-                    }
-            };
-            gather_k(ring[0]);
-
-            auto body = [&](int step, Codes &codes, const Codes &next) {
-                const int t0 = tile_at(step) * 32;
-                if (t0 + 32 > r.len) {
+                const int t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * 32;
+                if (t0 + 32 > pc.len) {
                     // Codes behind the request's end may name anything, and a weight of zero times an infinity is none: they become the
                     // tile's first token's (a lane's run of eight keys ends at its first one, or does not begin).
 #pragma unroll
                     for (int n = 0; n < NSV; ++n) {
                         const unsigned own = codes.v[0][n][0] & 0xFFu;
-                        const auto x = __builtin_amdgcn_permlane32_swap(own, own, false, false);
-                        const uint32_t good = x[0] * 0x01010101u;
+                        const auto y = __builtin_amdgcn_permlane32_swap(own, own, false, false);
+                        const uint32_t good = y[0] * 0x01010101u;
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
 #pragma unroll
                             for (int d = 0; d < 2; ++d) {
-                                const int live = min(max(r.len - (t0 + 16 * k + 8 * lh + 4 * d), 0), 4);   // bytes that stay
+                                const int live = min(max(pc.len - (t0 + 16 * k + 8 * lh + 4 * d), 0), 4);   // bytes that stay
                                 const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << (8 * live)) - 1u;
                                 codes.v[k][n][d] = (codes.v[k][n][d] & mask) | (good & ~mask);
                             }
@@ -473,11 +616,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         s[e] = z - slope2 * fabsf((float)(pos - key));
                     }
                 }
-                if (!((t0 + 31 <= pos_f && t0 + 31 < r.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= r.prefix)) {
+                if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int key = t0 + 16 * (e >> 3) + 8 * lh + (e & 7);
-                        const bool see = (key <= see_to && key >= see_from) || key < r.prefix;
+                        const bool see = (key <= see_to && key >= see_from) || key < pc.prefix;
                         s[e] = see ? s[e] : -INFINITY;
                     }
                 }
@@ -486,8 +629,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
                 {
-                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-                    mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+                    mt = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
                 }
                 if (!MODS) mt *= a.scale2;
                 if (__ballot(mt > m_ref + kRise)) {
@@ -527,121 +670,121 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
                 fetch(step + NB, codes);
             };
-            for (int st = 0; st < steps; st += NB)
+            for (int round = pc.r0; round < pc.r1; round += NB)
 #pragma unroll
-                for (int u = 0; u < NB; ++u)
-                    if (st + u < steps) body(st + u, ring[u], ring[(u + 1) % NB]);
-        }
-        {
-            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
-            lsum = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-        }
+                for (int u = 0; u < NB; ++u, ++step) body(round + u, ring[u], ring[(u + 1) % NB]);
+            {
+                const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+                lsum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+            }
 
-        // join the wavefronts that share rows, in order of kw; group g of eight accumulators ends with wavefront g % ways
-        const bool whole = r0 == 0 && r1 == rounds;
-        float L = lsum, M = m_ref;
-        if (ways > 1) {
-            if (lh == 0) {
-                xm[wave * 32 + ln] = m_ref;
-                xl[wave * 32 + ln] = lsum;
-            }
-            __syncthreads();
-            const int w0 = wave - kw;
-            for (int k = 0; k < ways; ++k) M = fmaxf(M, xm[(w0 + k) * 32 + ln]);
-            L = 0.f;
-            for (int k = 0; k < ways; ++k) L += xl[(w0 + k) * 32 + ln] * __builtin_amdgcn_exp2f(xm[(w0 + k) * 32 + ln] - M);
-            const float f = __builtin_amdgcn_exp2f(m_ref - M);
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[k][e] *= f;
-        }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const size_t part = part_of(a, h, w, r0 > 0 ? 0 : 1);
-        const int prow = rt * 32 + ln;
-        if (!whole && valid && lh == 0 && kw == 0) {
-            float *st = part_stats<D>(a, part) + prow * 2;
-            st[0] = M;
-            st[1] = L;
-        }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int reg = CH == 4 ? 4 * (g >> 1) + 2 * (g & 1) + e / 4 : 4 * g + e / 2;
-                x[e] = o[e % CH][reg];
-            }
-            const bool owner = (g & (ways - 1)) == kw;
+            // join the wavefronts that share rows, in order of kw; group g of eight accumulators ends with wavefront g % ways
+            float L = lsum, M = m_ref;
             if (ways > 1) {
-                float4_t *mine = reinterpret_cast<float4_t *>(xs) + wave * 128;
-                if (!owner) {
-                    mine[lane] = float4_t{x[0], x[1], x[2], x[3]};
-                    mine[64 + lane] = float4_t{x[4], x[5], x[6], x[7]};
+                if (lh == 0) {
+                    xm[wave * 32 + ln] = m_ref;
+                    xl[wave * 32 + ln] = lsum;
                 }
                 __syncthreads();
-                if (owner) {
-                    float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    for (int k = 0; k < ways; ++k) {
-                        if (k == kw) {
+                float ms[kWaves], ls[kWaves];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) t[e] += x[e];
-                            continue;
-                        }
-                        const float4_t *from = reinterpret_cast<const float4_t *>(xs) + (wave - kw + k) * 128;
-                        const float4_t y0 = from[lane], y1 = from[64 + lane];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            t[e] += y0[e];
-                            t[4 + e] += y1[e];
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = t[e];
+                for (int k = 0; k < kWaves; ++k) {   // (past the rows' wavefronts: their first once more, without weight)
+                    const int from = (wave - kw + (k < ways ? k : 0)) * 32 + ln;
+                    ms[k] = xm[from];
+                    ls[k] = k < ways ? xl[from] : 0.f;
                 }
-                __syncthreads();
+                L = 0.f;
+#pragma unroll
+                for (int k = 0; k < kWaves; ++k) M = fmaxf(M, ms[k]);
+#pragma unroll
+                for (int k = 0; k < kWaves; ++k) L += ls[k] * __builtin_amdgcn_exp2f(ms[k] - M);
+                const float f = __builtin_amdgcn_exp2f(m_ref - M);
+#pragma unroll
+                for (int k = 0; k < CH; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[k][e] *= f;
             }
-            if (owner && valid) {
-                const int ch = CH == 4 ? 32 * (g >> 1) + 16 * lh + 8 * (g & 1) : 16 * g + 8 * lh;
-                if (whole) {
-                    half8_t y;
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            const size_t part = part_of(a, h, w, pc.r0 > 0 ? 0 : 1);
+            const int prow = rt * 32 + ln;
+            if (!pc.whole && valid && lh == 0 && kw == 0) {
+                float *st = part_stats<D>(a, part) + prow * 2;
+                st[0] = M;
+                st[1] = L;
+            }
+            auto group = [&](int g, float (&y)[8]) {   // eight consecutive channels
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = (half_t)(x[e] * inv);
-                    *reinterpret_cast<half8_t *>(a.out + (size_t)(r.first + i) * a.out_stride + (size_t)hq * D + ch) = y;
+                for (int e = 0; e < 8; ++e) y[e] = o[e % CH][CH == 4 ? 4 * (g >> 1) + 2 * (g & 1) + e / 4 : 4 * g + e / 2];
+            };
+            auto store = [&](int g, const float (&y)[8]) {
+                if (!valid) return;
+                const int ch = CH == 4 ? 32 * (g >> 1) + 16 * lh + 8 * (g & 1) : 16 * g + 8 * lh;
+                if (pc.whole) {
+                    half8_t z;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = (half_t)(y[e] * inv);
+                    *reinterpret_cast<half8_t *>(a.out + (size_t)(pc.first + i) * a.out_stride + (size_t)hq * D + ch) = z;
                 } else {
                     float4_t *to = reinterpret_cast<float4_t *>(part_sums<D>(a, part) + (size_t)prow * D + ch);
-                    to[0] = float4_t{x[0], x[1], x[2], x[3]};
-                    to[1] = float4_t{x[4], x[5], x[6], x[7]};
+                    to[0] = float4_t{y[0], y[1], y[2], y[3]};
+                    to[1] = float4_t{y[4], y[5], y[6], y[7]};
                 }
+            };
+            // AT: groups that the buffer holds at once, of the rows' lanes alone (32 / AT rows at most)
+            auto join = [&](auto at_once) {
+                constexpr int AT = decltype(at_once)::value, ROWS = 32 / AT;
+                float4_t *buf = reinterpret_cast<float4_t *>(xs);
+                const int slot = lh * ROWS + (ln & (ROWS - 1));   // of 2 ROWS
+                auto cell = [&](int w_, int g, int half) { return buf + ((w_ * AT + g % AT) * 2 + half) * 2 * ROWS + slot; };
+                const bool mine = ln < ROWS;
+#pragma unroll
+                for (int g0 = 0; g0 < NG; g0 += AT) {
+#pragma unroll
+                    for (int g = g0; g < g0 + AT && g < NG; ++g) {
+                        float y[8];
+                        group(g, y);
+                        if (mine && (g & (ways - 1)) != kw) {
+                            *cell(wave, g, 0) = float4_t{y[0], y[1], y[2], y[3]};
+                            *cell(wave, g, 1) = float4_t{y[4], y[5], y[6], y[7]};
+                        }
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int g = g0; g < g0 + AT && g < NG; ++g) {
+                        if (!mine || (g & (ways - 1)) != kw) continue;
+                        float y[8];
+                        group(g, y);
+                        float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                        for (int k0 = 0; k0 < ways; k0 += 2) {   // (ways is even)
+                            float4_t z[2][2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                z[k][0] = *cell(wave - kw + k0 + k, g, 0);
+                                z[k][1] = *cell(wave - kw + k0 + k, g, 1);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) t[e] += k0 + k == kw ? y[e] : z[k][e / 4][e % 4];
+                        }
+                        store(g, t);
+                    }
+                    if (g0 + AT < NG) __syncthreads();
+                }
+                __syncthreads();   // (the buffers are the next piece's)
+            };
+            if (ways == 1) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float y[8];
+                    group(g, y);
+                    store(g, y);
+                }
+            } else if (pc.rows - pc.row0 <= 4) {
+                join(std::integral_constant<int, 8>());
+            } else {
+                join(std::integral_constant<int, 1>());
             }
-        }
-    };
-
-    long long left = sh.u1 - sh.u0, x = sh.x;
-    int b = sh.b;
-    Request r = request_of(a, b);
-    while (true) {
-        const int k = (int)(x / r.C), from = (int)(x - (long long)k * r.C), take = (int)min((long long)(r.C - from), left), to = from + take;
-        const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
-        for (int piece = 0; piece < 2; ++piece) {
-            const int j = piece == 0 ? jl : k;
-            if (piece == 1 && j == jl) break;
-            const int off = piece == 0 ? 0 : nl, rounds = piece == 0 ? nl : block_rounds(a, r, k);
-            int r0 = max(from - off, 0), r1 = to == r.C ? rounds : min(to - off, rounds);
-            if (!a.cut) {   // whole blocks, with the share that they begin in
-                const bool mine = off >= from && (off < to || to == r.C);
-                r0 = 0;
-                r1 = mine ? rounds : 0;
-            }
-            if (r0 < r1) run_block(r, b, j, r0, r1, rounds);
-        }
-        left -= take;
-        x += take;
-        if (left <= 0) break;
-        if (x == (long long)r.items * r.C) {
-            x = 0;
-            do r = request_of(a, ++b);   // (requests without new tokens have no rounds; the share's end lies before the last request's)
-            while (r.blocks == 0);
         }
     }
 }
@@ -690,7 +833,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedArgs a) {
         half8_t y;
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = (half_t)(x[e] * inv);
-        const int i = row / a.group, hq = h * a.group + (row - i * a.group);
+        const int i = token_of(a, row), hq = h * a.group + (row - i * a.group);
         *reinterpret_cast<half8_t *>(a.out + (size_t)(r.first + i) * a.out_stride + (size_t)hq * D + ch) = y;
     }
 }
@@ -755,6 +898,9 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.B = b->B;
     a.H = kv->H;
     a.group = b->Hq / kv->H;
+    a.group_shift = 31;
+    while ((1ll << (a.group_shift - 31)) < a.group) ++a.group_shift;
+    a.group_inverse = (unsigned)(((1ull << a.group_shift) + a.group - 1) / a.group);
     a.E = kv->n_entries;
     a.G = kv->cb_groups;
     a.pg_shift = __builtin_ctz(kv->D / kv->v / kv->cb_groups);
