@@ -211,7 +211,6 @@ __device__ __forceinline__ long long shfl_ll(long long v, int from) {
 // one writes it.  Returns the pieces; *rounds: theirs, each piece's rounded up to PAD.
 template <int PAD>
 __device__ __forceinline__ int list_pieces(const PagedArgs &a, int *b, long long *x, long long *left, bool write, int *starts, Piece *list, int *rounds) {
-    static_assert((PAD & (PAD - 1)) == 0, "");
     const int lane = threadIdx.x & 63;
     Request r = {};
     if (*b + lane < a.B) r = request_of(a, *b + lane);
@@ -275,7 +274,7 @@ __device__ __forceinline__ int list_pieces(const PagedArgs &a, int *b, long long
     }
     there = there && pc.r0 < pc.r1;
     pc.whole = pc.r0 == 0 && pc.r1 == n;
-    const int mine = there ? (pc.r1 - pc.r0 + PAD - 1) & -PAD : 0;
+    const int mine = there ? (pc.r1 - pc.r0 + PAD - 1) / PAD * PAD : 0;
     int upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -416,8 +415,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr int CPS = 8 / V;                   // K codes of a step
     constexpr int NSV = CH > V ? CH / V : 1;     // positions of a lane's V channels
     constexpr int VR = 2 * (V < CH ? V : CH);    // bytes of a gather
-    constexpr int NB = V == 2 ? 2 : 4;           // tiles of codes in flight
+    constexpr int NB = V == 2 ? 3 : 4;           // tiles of codes in flight
     constexpr int NG = D / 16;                   // groups of eight accumulators
+    constexpr int KN = NC * CPS, VN = 8 * NSV;   // gathers of a tile's keys, of a block's values, per lane
     extern __shared__ __align__(16) unsigned char smem[];   // (from LDS address 0: kernel_setup checks that)
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -507,26 +507,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             __syncthreads();
             staged = true;
         }
-        // K entries of the next tile as operands (each tile's gathers are requested a tile ahead)
+        // K entries of a tile as operands: one gather
         V16 kop[NC];
-        auto gather_k = [&](const Codes &codes) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int n = 0; n < CPS; ++n) {
-                    const int at = c * CPS + n;
-                    const uint32_t word = codes.k[at / 4];
-                    unsigned addr;
-                    if constexpr (COPIES) {
-                        addr = (at & 3) == 0 ? row_address<0>(word, k_const) : (at & 3) == 1 ? row_address<1>(word, k_const)
-                               : (at & 3) == 2 ? row_address<2>(word, k_const) : row_address<3>(word, k_const);
-                    } else {
-                        addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
-                    }
-                    lds_read<ES>(addr, &kop[c].w[n * (ES / 4)]);
-                }
+        auto gather_k = [&](const Codes &codes, int at) {
+            const uint32_t word = codes.k[at / 4];
+            unsigned addr;
+            if constexpr (COPIES) {
+                addr = (at & 3) == 0 ? row_address<0>(word, k_const) : (at & 3) == 1 ? row_address<1>(word, k_const)
+                       : (at & 3) == 2 ? row_address<2>(word, k_const) : row_address<3>(word, k_const);
+            } else {
+                addr = ((word >> (8 * (at & 3))) & 0xFFu) * ES + k_const + (unsigned)(at * 256 * ES);
+            }
+            lds_read<ES>(addr, &kop[at / CPS].w[at % CPS * (ES / 4)]);
         };
-        gather_k(ring[0]);
 
         int step = 0;
         for (int piece = 0; piece < pieces; ++piece) {
@@ -559,14 +552,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             const float slope2 = MODS && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
             const int see_to = min(pos, pc.len - 1), see_from = a.window > 0 ? pos - a.window + 1 : INT_MIN;
 
-            auto body = [&](int round, Codes &codes, const Codes &next) {
-                const int idx = (round << pc.log_ways) + kw;
-                if (idx >= count || round >= pc.r1) {   // (nothing for these rows in this round)
-                    gather_k(next);
-                    fetch(step + NB, codes);
-                    return;
-                }
-                const int t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * 32;
+            // This wavefront's tiles: idx0, idx0 + ways, ...
+            const int idx0 = (pc.r0 << pc.log_ways) + kw, rounds = pc.r1 - pc.r0;
+            const int tiles = min(max((count - idx0 + ways - 1) >> pc.log_ways, 0), rounds);
+            // The scores of a tile are formed while the weights of the tile before it are: s holds a tile's, next the following one's.
+            float16_t s, next;
+            if (tiles > 0) {
+#pragma unroll
+                for (int n = 0; n < KN; ++n) gather_k(ring[0], n);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kop[c].h8, qf[c], s, 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < KN / 2; ++n) gather_k(ring[1], n);
+            }
+            auto body = [&](int tile, Codes &codes, const Codes &after, const Codes &second) {
+                const int idx = idx0 + (tile << pc.log_ways), t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * 32;
                 if (t0 + 32 > pc.len) {
                     // Codes behind the request's end may name anything, and a weight of zero times an infinity is none: they become the
                     // tile's first token's (a lane's run of eight keys ends at its first one, or does not begin).
@@ -585,29 +587,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                             }
                     }
                 }
-                uint32_t g[2][8][CH / 2];   // channel pairs of the lane's eight keys of a block
-                auto gather_v = [&](int k) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int n = 0; n < NSV; ++n) {
-                            const uint32_t word = codes.v[k][n][e / 4];
-                            const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
-                                                  : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
-                            lds_read<VR>(addr + (unsigned)(n * VR), &g[k][e][n * (VR / 4)]);
-                        }
-                };
-                __builtin_amdgcn_sched_barrier(0);
-                // scores; the first values' gathers run beside them, the next tile's keys' behind them
-                float16_t s;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kop[c].h8, qf[c], s, 0, 0, 0);
-                gather_v(0);
-                __builtin_amdgcn_sched_barrier(0);
-                gather_k(next);
-                __builtin_amdgcn_sched_barrier(0);
                 if constexpr (MODS) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -624,17 +603,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         s[e] = see ? s[e] : -INFINITY;
                     }
                 }
-                // running maximum
+                // running maximum (a NaN raises nothing: its row's weights are NaN by themselves)
                 float mt = s[0];
 #pragma unroll
-                for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+                for (int e = 1; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, s[e]);
                 {
                     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-                    mt = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+                    mt = __builtin_elementwise_maximum(__uint_as_float(y[0]), __uint_as_float(y[1]));
                 }
                 if (!MODS) mt *= a.scale2;
                 if (__ballot(mt > m_ref + kRise)) {
-                    const float m_new = fmaxf(m_ref, mt), f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                    const float m_new = mt > m_ref ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
                     lsum *= f;
 #pragma unroll
@@ -643,36 +622,70 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         for (int e = 0; e < 16; ++e) o[k][e] *= f;
                 }
                 const float sub = kHeadroom - m_ref;
+
+                uint32_t g[2][8][CH / 2];   // channel pairs of the lane's eight keys of a block
+                auto gather_v = [&](int k, int at) {
+                    const int e = at / NSV, n = at % NSV;
+                    const uint32_t word = codes.v[k][n][e / 4];
+                    const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
+                                          : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
+                    lds_read<VR>(addr + (unsigned)(n * VR), &g[k][e][n * (VR / 4)]);
+                };
+                // A matrix instruction at a time with the vector instructions of its 32 clocks, and the gathers some 130 clocks ahead of
+                // their use: in bursts they overrun the counter of outstanding reads (15), and a wait for an old one waits for new ones.
+                __builtin_amdgcn_sched_barrier(0);
+                V16 pf[2];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    V16 pf;
+                for (int e = 0; e < 16; ++e) next[e] = 0.f;
+                constexpr int EW = 16 / NC, Q = NC / 4;   // weights per step, steps of a quarter
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(MODS ? s[8 * k + e] + sub : __builtin_fmaf(s[8 * k + e], a.scale2, sub));
-                        const float p1 = __builtin_amdgcn_exp2f(MODS ? s[8 * k + e + 1] + sub : __builtin_fmaf(s[8 * k + e + 1], a.scale2, sub));
-                        lsum += p0;
-                        lsum += p1;
-                        const half2_t p2 = {(half_t)p0, (half_t)p1};
-                        pf.h2[e / 2] = p2;
+                for (int c = 0; c < NC; ++c) {   // scores of the next tile; weights of this one
+                    next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kop[c].h8, qf[c], next, 0, 0, 0);
+                    if (c < Q) {
+#pragma unroll
+                        for (int n = 0; n < KN / 2 / Q; ++n) gather_k(after, KN / 2 + c * (KN / 2 / Q) + n);
+                    } else if (c < 3 * Q) {
+#pragma unroll
+                        for (int n = 0; n < VN / (2 * Q); ++n) gather_v(0, (c - Q) * (VN / (2 * Q)) + n);
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < VN / (2 * Q); ++n) gather_v(1, (c - 3 * Q) * (VN / (2 * Q)) + n);
                     }
 #pragma unroll
-                    for (int c = 0; c < CH / 2; ++c) {
-                        V16 lo, hi;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            lo.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][c], g[k][2 * e][c], 0x05040100u);
-                            hi.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][c], g[k][2 * e][c], 0x07060302u);
-                        }
-                        o[2 * c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo.h8, pf.h8, o[2 * c], 0, 0, 0);
-                        o[2 * c + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi.h8, pf.h8, o[2 * c + 1], 0, 0, 0);
+                    for (int e = c * EW; e < (c + 1) * EW; e += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(MODS ? s[e] + sub : __builtin_fmaf(s[e], a.scale2, sub));
+                        const float p1 = __builtin_amdgcn_exp2f(MODS ? s[e + 1] + sub : __builtin_fmaf(s[e + 1], a.scale2, sub));
+                        const half2_t p2 = {(half_t)p0, (half_t)p1}, one = {(half_t)1.f, (half_t)1.f};
+                        pf[e / 8].h2[e % 8 / 2] = p2;
+                        lsum = dot2(p2, one, lsum);
                     }
-                    if (k == 0) gather_v(1);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                fetch(step + NB, codes);
-            };
-            for (int round = pc.r0; round < pc.r1; round += NB)
+                constexpr int R = CH / 2;                 // steps of a quarter of the product with V
 #pragma unroll
-                for (int u = 0; u < NB; ++u, ++step) body(round + u, ring[u], ring[(u + 1) % NB]);
+                for (int m = 0; m < 2 * CH; ++m) {
+                    const int k = m / CH, f = m % CH;
+                    V16 op;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) op.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][f / 2], g[k][2 * e][f / 2], f & 1 ? 0x07060302u : 0x05040100u);
+                    o[f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op.h8, pf[k].h8, o[f], 0, 0, 0);
+                    if (m < R) {
+#pragma unroll
+                        for (int n = 0; n < VN / 2 / R; ++n) gather_v(1, VN / 2 + m * (VN / 2 / R) + n);
+                    } else if (m < 3 * R) {
+#pragma unroll
+                        for (int n = 0; n < KN / 2 / (2 * R); ++n) gather_k(second, (m - R) * (KN / 2 / (2 * R)) + n);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                s = next;
+            };
+            for (int tile = 0; tile < rounds; tile += NB)
+#pragma unroll
+                for (int u = 0; u < NB; ++u, ++step) {
+                    if (tile + u < tiles) body(tile + u, ring[u], ring[(u + 1) % NB], ring[(u + 2) % NB]);
+                    fetch(step + NB, ring[u]);
+                }
             {
                 const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
                 lsum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
