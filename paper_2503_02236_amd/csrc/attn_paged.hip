@@ -39,7 +39,8 @@ constexpr int kJoinOff = 2 * kSide;           // sums of wavefronts that share r
 constexpr int kStatOff = kJoinOff + 16384;    // their maxima and sums of weights, [wave][32] each
 constexpr int kScanOff = kStatOff + 2048;
 constexpr int kListOff = kScanOff + 256;      // pieces of the share, 64 at a time: their first rounds, and a Piece each
-constexpr int kLds = kListOff + 256 + 64 * 64;
+constexpr int kBaseOff = kListOff + 256 + 64 * 64;   // where the codes of the next rounds lie, [wave][64]
+constexpr int kLds = kBaseOff + kWaves * 64 * 8;
 constexpr float kHeadroom = 6.f, kRise = 8.f; // (log2)
 
 struct PagedArgs {
@@ -329,6 +330,12 @@ __device__ __forceinline__ void lds_read(unsigned addr, uint32_t *to) {
     const raw_t r = *reinterpret_cast<const __attribute__((address_space(3))) raw_t *>((uintptr_t)addr);
     __builtin_memcpy(to, &r, BYTES);
 }
+// ds_read_b64_tr_b16: of each group of 16 lanes, lane l gets half l % 4 of what lanes l / 4, 4 + l / 4, 8 + l / 4 and 12 + l / 4 ask for
+__device__ __forceinline__ void lds_read_transposed(unsigned addr, uint32_t *to) {
+    typedef short raw_t __attribute__((ext_vector_type(4)));
+    const raw_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<raw_t __attribute__((address_space(3))) *>((uintptr_t)addr));
+    __builtin_memcpy(to, &r, 8);
+}
 template <int BYTES>
 __device__ __forceinline__ typename Raw<BYTES>::type global_read(const void *p) {
     return *reinterpret_cast<const typename Raw<BYTES>::type *>(p);
@@ -340,22 +347,18 @@ __device__ __forceinline__ unsigned row_address(uint32_t w, unsigned lane_const)
     return __builtin_amdgcn_perm(w, lane_const, 0x0c020000u | ((4u + B) << 8));
 }
 
-// Codebooks of head h to LDS.  Rows of entries that do not exist are zero.
+// One side's codebooks of a head (cb) to LDS, for gathers of whole entries: every entry 256 / (2 v) times in a row of 256 bytes, or a
+// table per sub-vector.  Rows of entries that do not exist are zero.
 template <int D, int V, bool COPIES>
-__device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned char *smem, int tid) {
+__device__ __forceinline__ void stage_entries(const PagedArgs &a, const unsigned char *cb, unsigned char *to, int tid) {
     constexpr int ES = 2 * V, P = D / V;
-    const unsigned char *kc = reinterpret_cast<const unsigned char *>(a.k_cb) + (size_t)h * a.G * a.E * ES;
-    const unsigned char *vc = reinterpret_cast<const unsigned char *>(a.v_cb) + (size_t)h * a.G * a.E * ES;
     typedef typename Raw<ES>::type entry_t;
     const entry_t none = {};
     if constexpr (COPIES) {
         constexpr int N = 256 * 16 / kThreads;      // units of 16 bytes
         entry_t e[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int row = (tid + i * kThreads) >> 4;
-            e[i] = global_read<ES>(kc + (unsigned)(min(row, a.E - 1) * ES));
-        }
+        for (int i = 0; i < N; ++i) e[i] = global_read<ES>(cb + (unsigned)(min((tid + i * kThreads) >> 4, a.E - 1) * ES));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             entry_t r[16 / ES];
@@ -363,7 +366,7 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
             for (int k = 0; k < 16 / ES; ++k) r[k] = ((tid + i * kThreads) >> 4) < a.E ? e[i] : none;
             uint4 u;
             __builtin_memcpy(&u, r, 16);
-            reinterpret_cast<uint4 *>(smem)[tid + i * kThreads] = u;
+            reinterpret_cast<uint4 *>(to)[tid + i * kThreads] = u;
         }
     } else {
         constexpr int N = P * 256 / kThreads;
@@ -371,11 +374,16 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = tid + i * kThreads, row = u & 255, p = u >> 8;
-            e[i] = global_read<ES>(kc + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES));
+            e[i] = global_read<ES>(cb + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES));
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(smem)[tid + i * kThreads] = ((tid + i * kThreads) & 255) < a.E ? e[i] : none;
+        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(to)[tid + i * kThreads] = ((tid + i * kThreads) & 255) < a.E ? e[i] : none;
     }
+}
+// The same for gathers by channel position (v = 2): row e holds entry e for all 32 positions of the operand.
+template <int D, int V, bool COPIES>
+__device__ __forceinline__ void stage_positions(const PagedArgs &a, const unsigned char *cb, unsigned char *to, int tid) {
+    constexpr int ES = 2 * V;
     constexpr int CH = D / 32, US = 2 * (V < CH ? V : CH), UNITS = 2 * D / US;   // parts of an entry that one lane takes
     constexpr int N = 256 * UNITS / kThreads;
     typedef typename Raw<US>::type unit_t;
@@ -396,13 +404,13 @@ __device__ __forceinline__ void stage_tables(const PagedArgs &a, int h, unsigned
         int row, unit;
         place(i, &row, &unit);
         const int ch = unit * (US / 2), p = ch / V;
-        e[i] = global_read<US>(vc + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES + (ch % V) * 2));
+        e[i] = global_read<US>(cb + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES + (ch % V) * 2));
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         int row, unit;
         place(i, &row, &unit);
-        *reinterpret_cast<unit_t *>(smem + kSide + row * 256 + unit * US) = row < a.E ? e[i] : zero;
+        *reinterpret_cast<unit_t *>(to + row * 256 + unit * US) = row < a.E ? e[i] : zero;
     }
 }
 
@@ -413,11 +421,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr int NC = D / 16;                   // steps of the product with K
     constexpr int KW = P / 8;                    // dwords of a lane's K codes: half a token's
     constexpr int CPS = 8 / V;                   // K codes of a step
-    constexpr int NSV = CH > V ? CH / V : 1;     // positions of a lane's V channels
-    constexpr int VR = 2 * (V < CH ? V : CH);    // bytes of a gather
+    constexpr bool TR = V >= 4;                  // V by transposing reads
+    constexpr int NR = TR ? CH * 4 / V : CH / V; // positions of a lane's V codes
+    constexpr int VW = TR ? NR : NR * 4;         // dwords of them: four or sixteen keys each
     constexpr int NB = V == 2 ? 3 : 4;           // tiles of codes in flight
     constexpr int NG = D / 16;                   // groups of eight accumulators
-    constexpr int KN = NC * CPS, VN = 8 * NSV;   // gathers of a tile's keys, of a block's values, per lane
+    constexpr int KN = NC * CPS, VN = TR ? 2 * CH : 8 * NR;   // gathers of a lane: of a tile's keys, of 16 keys' values
     extern __shared__ __align__(16) unsigned char smem[];   // (from LDS address 0: kernel_setup checks that)
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -429,12 +438,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (!find_share<kThreads>(a, w, reinterpret_cast<long long *>(smem + kScanOff), &sh)) return;
 
     const int ps_mask = (1 << a.log_ps) - 1;
+    // TR: the position block of a lane's V codes and its keys among the 16 of its half
+    const int c0 = 4 * ((lane >> 4) & 1) + (lane & 3), e0 = (lane >> 2) & 3;
     // lane constants of the gathers
-    const unsigned k_const = COPIES ? (unsigned)((V == 2 ? lane : V == 4 ? ln : ln & 15) * ES) : (unsigned)(lh * (P / 2) * 256 * ES);
-    const unsigned v_const = (unsigned)kSide + (unsigned)(ln * CH * 2);
-    // offsets of the lane's codes in a block of 16 tokens
-    const int key16 = 8 * ((ln >> 2) & 1) + 4 * ((ln >> 3) & 1) + (ln & 3);
-    const unsigned k_off = (unsigned)(key16 * P + lh * (P / 2)), v_off = (unsigned)(ln * CH / V * 16 + lh * 8);
+    const unsigned copy = (unsigned)((V == 2 ? lane : V == 4 ? ln : ln & 15) * ES);
+    const unsigned k_const = COPIES ? copy : (unsigned)(lh * (P / 2) * 256 * ES);
+    const unsigned v_const = (unsigned)kSide + (!TR ? (unsigned)(ln * CH * 2) : COPIES ? copy : (unsigned)(c0 * NR * 256 * ES));
+    // where the lane's codes lie in a block of 16 tokens
+    const uint8_t *const k_lane = a.k_codes + ((4 * (ln & 3) + (ln >> 3)) * P + lh * (P / 2));
+    const uint8_t *const v_lane = a.v_codes + (TR ? c0 * NR * 16 + 4 * e0 : ln * NR * 16);
+    size_t *const bases = reinterpret_cast<size_t *>(smem + kBaseOff) + wave * 64;
+    const size_t *const k_bases = bases + ((ln >> 2) & 1), *const v_bases = bases + lh;
     float *xs = reinterpret_cast<float *>(smem + kJoinOff), *xm = reinterpret_cast<float *>(smem + kStatOff), *xl = xm + kWaves * 32;
     int *starts = reinterpret_cast<int *>(smem + kListOff);
     Piece *list = reinterpret_cast<Piece *>(smem + kListOff + 256);
@@ -464,46 +478,43 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             next_id = a.table[(size_t)pc.b * a.max_pages + (max(min(at, pc.len - 1), 0) >> a.log_ps)];
             next_off = (at & ps_mask) * P;
         };
+        auto write_bases = [&]() { bases[lane] = (((size_t)min(max(next_id, 0), a.n_pages - 1) * a.H + h) << a.log_ps) * P + (size_t)next_off; };
         page_ids(0);
-        size_t bases = 0;
+        write_bases();
+        page_ids(32);
+        size_t k_base = k_bases[0], v_base = v_bases[0];
         struct Codes {
-            uint32_t k[KW], v[2][NSV][2];
+            uint32_t k[KW], v[VW];
         } ring[NB];
         auto fetch = [&](int step, Codes &c) {
-            if ((step & 31) == 0) {
-                bases = (((size_t)min(max(next_id, 0), a.n_pages - 1) * a.H + h) << a.log_ps) * P + (size_t)next_off;
-                page_ids(step + 32);
-            }
-            size_t base[2];
+            constexpr int KB = KW >= 4 ? 16 : KW * 4, VB = TR ? 4 : 16;
+            const uint8_t *kp = k_lane + k_base, *vp = v_lane + v_base;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int from = 2 * (step & 31) + k;
-                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bases, from);
-                const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(bases >> 32), from);
-                base[k] = ((size_t)hi << 32) | lo;
-            }
-            const uint8_t *kp = a.k_codes + (ln < 16 ? base[0] : base[1]) + k_off;
-            constexpr int BYTES = KW >= 4 ? 16 : KW * 4;
-#pragma unroll
-            for (int n = 0; n < KW; n += BYTES / 4) {
-                const typename Raw<BYTES>::type u = global_read<BYTES>(kp + 4 * n);
-                __builtin_memcpy(&c.k[n], &u, BYTES);
+            for (int n = 0; n < KW; n += KB / 4) {
+                const typename Raw<KB>::type u = global_read<KB>(kp + 4 * n);
+                __builtin_memcpy(&c.k[n], &u, KB);
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int n = 0; n < NSV; ++n) {
-                    const Raw<8>::type u = global_read<8>(a.v_codes + base[k] + v_off + 16 * n);
-                    c.v[k][n][0] = u.x;
-                    c.v[k][n][1] = u.y;
-                }
+            for (int n = 0; n < NR; ++n) {
+                const typename Raw<VB>::type u = global_read<VB>(vp + 16 * n);
+                __builtin_memcpy(&c.v[n * (VB / 4)], &u, VB);
+            }
+            if (((step + 1) & 31) == 0) {
+                write_bases();
+                page_ids(step + 33);
+            }
+            k_base = k_bases[2 * ((step + 1) & 31)];
+            v_base = v_bases[2 * ((step + 1) & 31)];
         };
 #pragma unroll
         for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
         if (!staged) {   // (while the first codes are on their way)
             int t = tid;
             asm volatile("" : "+v"(t));   // (or its addresses are formed before the loop, and lie in scratch)
-            stage_tables<D, V, COPIES>(a, h, smem, t);
+            const size_t cb = (size_t)h * a.G * a.E * ES;
+            stage_entries<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.k_cb) + cb, smem, t);
+            if constexpr (TR) stage_entries<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.v_cb) + cb, smem + kSide, t);
+            else stage_positions<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.v_cb) + cb, smem + kSide, t);
             __syncthreads();
             staged = true;
         }
@@ -556,8 +567,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             const int idx0 = (pc.r0 << pc.log_ways) + kw, rounds = pc.r1 - pc.r0;
             const int tiles = min(max((count - idx0 + ways - 1) >> pc.log_ways, 0), rounds);
             // The scores of a tile are formed while the weights of the tile before it are: s holds a tile's, next the following one's.
-            float16_t s, next;
+            float16_t scores[2];
+            const float scale2 = [&] {
+                float x = a.scale2;
+                asm("" : "+v"(x));   // (a product and sum with a scalar operand takes twice as long)
+                return x;
+            }();
             if (tiles > 0) {
+                float16_t &s = scores[0];
 #pragma unroll
                 for (int n = 0; n < KN; ++n) gather_k(ring[0], n);
 #pragma unroll
@@ -567,38 +584,35 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int n = 0; n < KN / 2; ++n) gather_k(ring[1], n);
             }
-            auto body = [&](int tile, Codes &codes, const Codes &after, const Codes &second) {
+            auto body = [&](int tile, float16_t &s, float16_t &next, Codes &codes, const Codes &after, const Codes &second) {
                 const int idx = idx0 + (tile << pc.log_ways), t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * 32;
                 if (t0 + 32 > pc.len) {
                     // Codes behind the request's end may name anything, and a weight of zero times an infinity is none: they become the
-                    // tile's first token's (a lane's run of eight keys ends at its first one, or does not begin).
+                    // tile's first token's.
 #pragma unroll
-                    for (int n = 0; n < NSV; ++n) {
-                        const unsigned own = codes.v[0][n][0] & 0xFFu;
-                        const auto y = __builtin_amdgcn_permlane32_swap(own, own, false, false);
-                        const uint32_t good = y[0] * 0x01010101u;
+                    for (int n = 0; n < NR; ++n) {
+                        const uint32_t good = (__shfl((int)codes.v[TR ? n : 4 * n], TR ? lane & 19 : ln, 64) & 0xFF) * 0x01010101u;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
-#pragma unroll
-                            for (int d = 0; d < 2; ++d) {
-                                const int live = min(max(pc.len - (t0 + 16 * k + 8 * lh + 4 * d), 0), 4);   // bytes that stay
-                                const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << (8 * live)) - 1u;
-                                codes.v[k][n][d] = (codes.v[k][n][d] & mask) | (good & ~mask);
-                            }
+                        for (int d = 0; d < VW / NR; ++d) {
+                            const int live = min(max(pc.len - (t0 + 16 * lh + 4 * (TR ? e0 : d)), 0), 4);   // bytes that stay
+                            const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << (8 * live)) - 1u;
+                            uint32_t &word = codes.v[n * (VW / NR) + d];
+                            word = (word & mask) | (good & ~mask);
+                        }
                     }
                 }
                 if constexpr (MODS) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         float z = a.cap_out > 0.f ? a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f) : s[e] * a.scale2;
-                        const int key = t0 + 16 * (e >> 3) + 8 * lh + (e & 7);
+                        const int key = t0 + 16 * lh + 4 * (e & 3) + (e >> 2);
                         s[e] = z - slope2 * fabsf((float)(pos - key));
                     }
                 }
                 if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int key = t0 + 16 * (e >> 3) + 8 * lh + (e & 7);
+                        const int key = t0 + 16 * lh + 4 * (e & 3) + (e >> 2);
                         const bool see = (key <= see_to && key >= see_from) || key < pc.prefix;
                         s[e] = see ? s[e] : -INFINITY;
                     }
@@ -611,7 +625,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
                     mt = __builtin_elementwise_maximum(__uint_as_float(y[0]), __uint_as_float(y[1]));
                 }
-                if (!MODS) mt *= a.scale2;
+                if (!MODS) mt *= scale2;
                 if (__ballot(mt > m_ref + kRise)) {
                     const float m_new = mt > m_ref ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
@@ -623,13 +637,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
                 const float sub = kHeadroom - m_ref;
 
-                uint32_t g[2][8][CH / 2];   // channel pairs of the lane's eight keys of a block
+                // Values of 16 keys, k of the two steps: operands as they come (TR), or channel pairs of the lane's eight keys.
+                // TR: lane 4 e + c of a group of 16 asks for the entry of key 16 lh + 4 e + 2 k + j and position block c, part f; the
+                // transposing read gives lane l the four keys e of channel l % 4 of block l / 4.
+                V16 vop[2][TR ? CH : 1];
+                uint32_t g[2][8][TR ? 1 : CH / 2];
                 auto gather_v = [&](int k, int at) {
-                    const int e = at / NSV, n = at % NSV;
-                    const uint32_t word = codes.v[k][n][e / 4];
-                    const unsigned addr = (e & 3) == 0 ? row_address<0>(word, v_const) : (e & 3) == 1 ? row_address<1>(word, v_const)
-                                          : (e & 3) == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
-                    lds_read<VR>(addr + (unsigned)(n * VR), &g[k][e][n * (VR / 4)]);
+                    auto address = [&](uint32_t word, int byte) {
+                        if constexpr (!TR || COPIES)
+                            return byte == 0 ? row_address<0>(word, v_const) : byte == 1 ? row_address<1>(word, v_const)
+                                   : byte == 2 ? row_address<2>(word, v_const) : row_address<3>(word, v_const);
+                        else return ((word >> (8 * byte)) & 0xFFu) * ES + v_const;
+                    };
+                    if constexpr (TR) {
+                        const int f = at / 2, j = at % 2, n = f * 4 / V;
+                        lds_read_transposed(address(codes.v[n], 2 * k + j) + (unsigned)((COPIES ? 0 : n * 256 * ES) + (f * 4 % V) * 2), &vop[k][f].w[2 * j]);
+                    } else {   // slot 4 j + e of the eight is key 4 e + 2 k + j of the 16
+                        const int i = at / NR, n = at % NR;
+                        lds_read<2 * V>(address(codes.v[4 * n + (i & 3)], 2 * k + (i >> 2)) + (unsigned)(n * 2 * V), &g[k][i][n * (V / 2)]);
+                    }
                 };
                 // A matrix instruction at a time with the vector instructions of its 32 clocks, and the gathers some 130 clocks ahead of
                 // their use: in bursts they overrun the counter of outstanding reads (15), and a wait for an old one waits for new ones.
@@ -653,8 +679,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     }
 #pragma unroll
                     for (int e = c * EW; e < (c + 1) * EW; e += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(MODS ? s[e] + sub : __builtin_fmaf(s[e], a.scale2, sub));
-                        const float p1 = __builtin_amdgcn_exp2f(MODS ? s[e + 1] + sub : __builtin_fmaf(s[e + 1], a.scale2, sub));
+                        const float p0 = __builtin_amdgcn_exp2f(MODS ? s[e] + sub : __builtin_fmaf(s[e], scale2, sub));
+                        const float p1 = __builtin_amdgcn_exp2f(MODS ? s[e + 1] + sub : __builtin_fmaf(s[e + 1], scale2, sub));
                         const half2_t p2 = {(half_t)p0, (half_t)p1}, one = {(half_t)1.f, (half_t)1.f};
                         pf[e / 8].h2[e % 8 / 2] = p2;
                         lsum = dot2(p2, one, lsum);
@@ -666,8 +692,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 for (int m = 0; m < 2 * CH; ++m) {
                     const int k = m / CH, f = m % CH;
                     V16 op;
+                    if constexpr (TR) {
+                        op = vop[k][f];
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) op.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][f / 2], g[k][2 * e][f / 2], f & 1 ? 0x07060302u : 0x05040100u);
+                        for (int e = 0; e < 4; ++e) op.w[e] = __builtin_amdgcn_perm(g[k][2 * e + 1][f / 2], g[k][2 * e][f / 2], f & 1 ? 0x07060302u : 0x05040100u);
+                    }
                     o[f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op.h8, pf[k].h8, o[f], 0, 0, 0);
                     if (m < R) {
 #pragma unroll
@@ -678,12 +708,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                s = next;
             };
             for (int tile = 0; tile < rounds; tile += NB)
 #pragma unroll
                 for (int u = 0; u < NB; ++u, ++step) {
-                    if (tile + u < tiles) body(tile + u, ring[u], ring[(u + 1) % NB], ring[(u + 2) % NB]);
+                    if (tile + u < tiles) {
+                        body(tile + u, scores[NB % 2 ? 0 : u % 2], scores[NB % 2 ? 1 : 1 - u % 2], ring[u], ring[(u + 1) % NB], ring[(u + 2) % NB]);
+                        if (NB % 2) scores[0] = scores[1];
+                    }
                     fetch(step + NB, ring[u]);
                 }
             {
@@ -727,7 +759,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             }
             auto group = [&](int g, float (&y)[8]) {   // eight consecutive channels
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = o[e % CH][CH == 4 ? 4 * (g >> 1) + 2 * (g & 1) + e / 4 : 4 * g + e / 2];
+                for (int e = 0; e < 8; ++e)
+                    y[e] = TR ? o[CH == 4 ? 2 * (g & 1) + e / 4 : e / 4][4 * (CH == 4 ? g >> 1 : g) + e % 4]
+                              : o[e % CH][CH == 4 ? 4 * (g >> 1) + 2 * (g & 1) + e / 4 : 4 * g + e / 2];
             };
             auto store = [&](int g, const float (&y)[8]) {
                 if (!valid) return;
