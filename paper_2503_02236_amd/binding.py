@@ -163,7 +163,8 @@ def marshal_built_for() -> tuple:
     """What the native marshalling has to have been built for: torch (whose tensors it reads by inlined accessors, so that a
     module for another build can load and read the wrong fields), Python, and the structs that it fills."""
     return ("torch %s %s hip %s python %s" % (torch.__version__, torch.version.git_version, torch.version.hip, sys.implementation.cache_tag),
-            ctypes.sizeof(vq_weight_t), ctypes.sizeof(vq_kv_t), ctypes.sizeof(vq_gemv_pack_t))
+            ctypes.sizeof(vq_weight_t), ctypes.sizeof(vq_kv_t), ctypes.sizeof(vq_gemv_pack_t), ctypes.sizeof(vq_kv_pages_t), ctypes.sizeof(vq_page_step_t),
+            ctypes.sizeof(vq_paged_batch_t))
 
 
 def _load_marshal(l) -> None:
@@ -176,8 +177,9 @@ def _load_marshal(l) -> None:
         return
     address = lambda name: ctypes.cast(getattr(l, name), ctypes.c_void_p).value  # noqa: E731
     native.init(tuple(address(n) for n in ("vq_gemv", "vq_gemv_workspace", "vq_gemv_batch", "vq_gemv_batch_workspace", "vq_gemm",
-                                           "vq_gemm_workspace", "vq_attn_decode", "vq_attn_decode_workspace", "vq_kv_quantize")),
-                VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError)
+                                           "vq_gemm_workspace", "vq_attn_decode", "vq_attn_decode_workspace", "vq_kv_quantize", "vq_kv_pages_assign",
+                                           "vq_kv_quantize_paged", "vq_attn_paged", "vq_attn_paged_workspace")),
+                VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError, VQKVPagesDev, VQPagePlan)
     _marshal = native
 
 
@@ -653,6 +655,10 @@ def vq_kv_pages_assign(new_lens: torch.Tensor, lens: torch.Tensor, block_table: 
                        n_free_out: Optional[torch.Tensor] = None) -> VQPagePlan:
     """Pages for the new tokens of every request, and the pages of ended ones back: updates block_table, free_pages and
     ``n_free_out`` (``n_free`` itself unless given), fills and returns ``plan`` (for ``n_tokens`` new tokens at most)."""
+    if _marshal is not None and plan is not None:
+        r = _marshal.kv_pages_assign(new_lens, lens, block_table, free_pages, n_free, page_tokens, plan, n_free_out)
+        if r is not NotImplemented:
+            return r
     B = new_lens.shape[0]
     if plan is None:
         if n_tokens is None:
@@ -674,6 +680,8 @@ def vq_kv_pages_assign(new_lens: torch.Tensor, lens: torch.Tensor, block_table: 
 
 def vq_kv_quantize_paged(kv: VQKVPagesDev, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantize new tokens (fp16 [tokens][H][D] each, tokens may lie apart) and store their codes at their slots (negative: skipped)."""
+    if _marshal is not None and _marshal.kv_quantize_paged(kv, k_new, v_new, slots) is not NotImplemented:
+        return
     d = kv.desc()
     kp, ks = _rows(k_new, "k_new", kv.H, kv.D)
     vp, vs = _rows(v_new, "v_new", kv.H, kv.D)
@@ -695,6 +703,10 @@ def vq_attn_paged(kv: VQKVPagesDev, q: torch.Tensor, sm_scale: float, block_tabl
                   slopes: Optional[torch.Tensor] = None, prefix_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[tokens][Hq][D]: attention of every request's new tokens (q, fp16, tokens may lie apart) over its pages, causal, optionally with
     a sliding ``window``, capped scores, a distance bias and a prefix that all of them attend."""
+    if _marshal is not None:
+        r = _marshal.attn_paged(kv, q, sm_scale, block_table, cu_new, seq_lens, out, ws, window, softcap, slopes, prefix_lens)
+        if r is not NotImplemented:
+            return r
     if out is None:
         out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
     qp, qs = _rows(q, "q", None, kv.D)

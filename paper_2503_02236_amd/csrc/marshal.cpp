@@ -1,5 +1,5 @@
-// Argument marshalling of the calls that a decode step makes by the hundred: vq_gemv, vq_gemv_batch, vq_gemm, vq_attn_decode and
-// vq_kv_quantize from Python objects to the C ABI.  What it does is what the functions of the same names in binding.py do by
+// Argument marshalling of the calls that a decode step makes by the hundred: vq_gemv, vq_gemv_batch, vq_gemm, vq_attn_decode,
+// vq_kv_quantize and their paged forms (vq_kv_pages_assign, vq_kv_quantize_paged, vq_attn_paged) from Python objects to the C ABI.  What it does is what the functions of the same names in binding.py do by
 // ctypes, object for object, and nothing else: every call reads and checks its arguments anew, nothing is kept.  Calls that
 // are not plain -- subclasses, tensors and modes that intercept calls, values that fail a check -- return NotImplemented,
 // and binding.py takes them its own way, error messages included.
@@ -33,10 +33,15 @@ struct Library {
     decltype(&vq_attn_decode) attn_decode;
     decltype(&vq_attn_decode_workspace) attn_decode_workspace;
     decltype(&vq_kv_quantize) kv_quantize;
+    decltype(&vq_kv_pages_assign) kv_pages_assign;
+    decltype(&vq_kv_quantize_paged) kv_quantize_paged;
+    decltype(&vq_attn_paged) attn_paged;
+    decltype(&vq_attn_paged_workspace) attn_paged_workspace;
 } lib;
-PyObject *weight_type, *kv_type, *pack_type, *error_type;
+PyObject *weight_type, *kv_type, *pack_type, *error_type, *pages_type, *plan_type;
 PyObject *s_N, *s_K, *s_v, *s_code_bits, *s_codes, *s_codebooks, *s_scale, *s_pack, *s_hot_entries, *s_cb_tile;
 PyObject *s_B, *s_H, *s_D, *s_T, *s_k_codes, *s_v_codes, *s_k_codebooks, *s_v_codebooks, *s_seq_lens;
+PyObject *s_page_tokens, *s_cu_new, *s_slots, *s_positions, *s_status;
 
 struct NotPlain {};   // thrown where binding.py has to take the call
 
@@ -69,14 +74,19 @@ int int_attr(PyObject *object, PyObject *name) {
 }
 
 // A tensor that is nothing but memory on the GPU.
-const at::Tensor &tensor(PyObject *o) {
+const at::Tensor &strided_tensor(PyObject *o) {
     if (!THPVariable_CheckExact(o)) throw NotPlain();
     const at::Tensor &t = THPVariable_Unpack(o);
     const auto keys = t.key_set();
-    if (!t.defined() || !t.is_cuda() || !t.has_storage() || t.layout() != at::kStrided || !t.is_contiguous() || keys.has(c10::DispatchKey::Python) ||
+    if (!t.defined() || !t.is_cuda() || !t.has_storage() || t.layout() != at::kStrided || keys.has(c10::DispatchKey::Python) ||
         keys.has(c10::DispatchKey::FuncTorchBatched) || keys.has(c10::DispatchKey::FuncTorchGradWrapper) || keys.has(c10::DispatchKey::Functionalize) ||
         keys.has(c10::DispatchKey::Conjugate) || keys.has(c10::DispatchKey::Negative) || keys.has(c10::DispatchKey::ZeroTensor))
         throw NotPlain();
+    return t;
+}
+const at::Tensor &tensor(PyObject *o) {
+    const at::Tensor &t = strided_tensor(o);
+    if (!t.is_contiguous()) throw NotPlain();
     return t;
 }
 void *data(PyObject *o, at::ScalarType type) {
@@ -175,6 +185,55 @@ vq_kv_t cache(PyObject *kv) {
     d.k_codebooks = data(kb.o, at::kHalf);
     d.v_codebooks = data(vb.o, at::kHalf);
     if (sl.o != Py_None) d.seq_lens = (const int *)data(sl.o, at::kInt);
+    return d;
+}
+
+// binding._here: a contiguous tensor of this type and shape on the device of the current stream
+void *here(PyObject *o, at::ScalarType type, at::IntArrayRef shape, int device) {
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != type || t.get_device() != device || t.sizes() != shape) throw NotPlain();
+    return t.data_ptr();
+}
+void *here_or_none(PyObject *o, at::ScalarType type, at::IntArrayRef shape, int device) { return o == Py_None ? nullptr : here(o, type, shape, device); }
+
+// binding._rows: fp16 [tokens][heads][D] whose tokens may lie apart
+struct Rows {
+    void *p;
+    size_t stride;
+    int64_t tokens, heads;
+    Rows(PyObject *o, int64_t D, int device) {
+        const at::Tensor &t = strided_tensor(o);
+        if (t.scalar_type() != at::kHalf || t.get_device() != device || t.dim() != 3 || t.size(2) != D || t.size(0) > INT_MAX || t.size(1) > INT_MAX) throw NotPlain();
+        if (t.numel() > 0 && (t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != D))) throw NotPlain();
+        tokens = t.size(0);
+        heads = t.size(1);
+        const int64_t step = tokens > 1 ? t.stride(0) : heads * D;
+        if (step < 0) throw NotPlain();
+        p = t.data_ptr();
+        stride = (size_t)step;
+    }
+};
+
+// VQKVPagesDev.desc()
+vq_kv_pages_t pages(PyObject *kv, int device) {
+    if ((PyObject *)Py_TYPE(kv) != pages_type) throw NotPlain();
+    vq_kv_pages_t d{};
+    d.H = int_attr(kv, s_H);
+    d.D = int_attr(kv, s_D);
+    d.v = int_attr(kv, s_v);
+    d.page_tokens = int_attr(kv, s_page_tokens);
+    if (d.D <= 0 || d.v <= 0 || d.page_tokens <= 0) throw NotPlain();
+    Ref kc(kv, s_k_codes), vc(kv, s_v_codes), kb(kv, s_k_codebooks), vb(kv, s_v_codebooks);
+    const at::Tensor &cb = tensor(kb.o), &codes = tensor(kc.o);
+    if (cb.dim() != 4 || cb.size(1) > INT_MAX || cb.size(2) > INT_MAX || codes.dim() != 4 || codes.size(0) > INT_MAX) throw NotPlain();
+    d.cb_groups = (int)cb.size(1);
+    d.n_entries = (int)cb.size(2);
+    d.n_pages = (int)codes.size(0);
+    const int64_t P = d.D / d.v;
+    d.k_codes = here(kc.o, at::kByte, {d.n_pages, d.H, d.page_tokens, P}, device);
+    d.v_codes = here(vc.o, at::kByte, {d.n_pages, d.H, d.page_tokens / 16, P, 16}, device);
+    d.k_codebooks = here(kb.o, at::kHalf, {d.H, d.cb_groups, d.n_entries, d.v}, device);
+    d.v_codebooks = here(vb.o, at::kHalf, {d.H, d.cb_groups, d.n_entries, d.v}, device);
     return d;
 }
 
@@ -369,12 +428,122 @@ PyObject *kv_quantize(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
-// (nine addresses, VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError)
+// (new_lens, lens, block_table, free_pages, n_free, page_tokens, plan, n_free_out or None)
+PyObject *kv_pages_assign(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        if (n != 8 || (PyObject *)Py_TYPE(args[6]) != plan_type) throw NotPlain();
+        const at::Tensor &table = tensor(args[2]), &lens = tensor(args[0]), &free_pages = tensor(args[3]);   // (on a GPU, so that there is a stream)
+        const auto current = c10::hip::getCurrentHIPStream();
+        const int device = current.device_index();
+        if (table.dim() != 2 || lens.dim() != 1 || free_pages.dim() != 1 || lens.size(0) > INT_MAX || table.size(1) > INT_MAX || free_pages.size(0) > INT_MAX)
+            throw NotPlain();
+        vq_page_step_t d{};
+        const int64_t B = lens.size(0), W = table.size(1), pool = free_pages.size(0);
+        auto i32 = [&](PyObject *o, int64_t size) { return (int *)here(o, at::kInt, {size}, device); };
+        Ref cu(args[6], s_cu_new), seq(args[6], s_seq_lens), slots(args[6], s_slots), positions(args[6], s_positions), status(args[6], s_status);
+        const at::Tensor &t = tensor(slots.o);
+        if (t.dim() != 1 || t.size(0) > INT_MAX) throw NotPlain();
+        const int64_t tokens = t.size(0);
+        d.B = (int)B;
+        d.max_pages = (int)W;
+        d.page_tokens = as_int(args[5]);
+        d.n_pages = (int)pool;
+        d.n_tokens = (int)tokens;
+        d.new_lens = i32(args[0], B);
+        d.lens = i32(args[1], B);
+        d.block_table = (int *)here(args[2], at::kInt, {B, W}, device);
+        d.free_pages = i32(args[3], pool);
+        d.n_free = i32(args[4], 1);
+        d.seq_lens = i32(seq.o, B);
+        d.n_free_out = i32(args[7] == Py_None ? args[4] : args[7], 1);
+        d.cu_new = i32(cu.o, B + 1);
+        d.slots = i32(slots.o, tokens);
+        d.positions = positions.o == Py_None ? nullptr : i32(positions.o, tokens);
+        d.status = i32(status.o, B);
+        void *s = (void *)current.stream();
+        int st;
+        VQ_WITHOUT_GIL(st, lib.kv_pages_assign(&d, s));
+        check(st, "vq_kv_pages_assign");
+        Py_INCREF(args[6]);
+        return args[6];
+    });
+}
+
+// (kv, k_new, v_new, slots)
+PyObject *kv_quantize_paged(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        if (n != 4) throw NotPlain();
+        strided_tensor(args[1]);   // (on a GPU, so that there is a stream)
+        const auto current = c10::hip::getCurrentHIPStream();
+        const int device = current.device_index();
+        const vq_kv_pages_t kv = pages(args[0], device);
+        const Rows k(args[1], kv.D, device), v(args[2], kv.D, device);
+        if (k.heads != kv.H || v.heads != kv.H || k.tokens != v.tokens) throw NotPlain();
+        const int *slots = (const int *)here(args[3], at::kInt, {k.tokens}, device);
+        void *s = (void *)current.stream();
+        int st;
+        VQ_WITHOUT_GIL(st, lib.kv_quantize_paged(&kv, k.p, k.stride, v.p, v.stride, slots, (int)k.tokens, s));
+        check(st, "vq_kv_quantize_paged");
+        Py_RETURN_NONE;
+    });
+}
+
+// (kv, q, sm_scale, block_table, cu_new, seq_lens, out or None, ws or None, window, softcap, slopes or None, prefix_lens or None)
+PyObject *attn_paged(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        if (n != 12 || !PyFloat_CheckExact(args[2]) || !PyFloat_CheckExact(args[9])) throw NotPlain();
+        no_modes();
+        strided_tensor(args[1]);   // (on a GPU, so that there is a stream)
+        const auto current = c10::hip::getCurrentHIPStream();
+        const int device = current.device_index();
+        const vq_kv_pages_t kv = pages(args[0], device);
+        const Rows q(args[1], kv.D, device);
+        const at::Tensor &table = tensor(args[3]);
+        if (table.dim() != 2 || table.size(0) > INT_MAX || table.size(1) > INT_MAX) throw NotPlain();
+        const int64_t B = table.size(0);
+        vq_paged_batch_t b{};
+        b.B = (int)B;
+        b.max_pages = (int)table.size(1);
+        b.n_tokens = (int)q.tokens;
+        b.Hq = (int)q.heads;
+        b.block_table = (const int *)here(args[3], at::kInt, {B, table.size(1)}, device);
+        b.cu_new = (const int *)here(args[4], at::kInt, {B + 1}, device);
+        b.seq_lens = (const int *)here(args[5], at::kInt, {B}, device);
+        b.window = as_int(args[8]);
+        b.softcap = (float)PyFloat_AS_DOUBLE(args[9]);
+        b.slopes = (const float *)here_or_none(args[10], at::kFloat, {q.heads}, device);
+        b.prefix_lens = (const int *)here_or_none(args[11], at::kInt, {B}, device);
+        const float sm_scale = (float)PyFloat_AS_DOUBLE(args[2]);
+        at::Tensor own;
+        void *out;
+        size_t out_stride = (size_t)(q.heads * kv.D);
+        if (args[6] == Py_None) {
+            own = at::empty({q.tokens, q.heads, (int64_t)kv.D}, strided_tensor(args[1]).options());
+            out = own.data_ptr();
+        } else {
+            const Rows o(args[6], kv.D, device);
+            if (o.tokens != q.tokens || o.heads != q.heads) throw NotPlain();
+            out = o.p;
+            out_stride = o.stride;
+        }
+        Workspace ws(args[7], strided_tensor(args[1]).device(), [&] { return lib.attn_paged_workspace(&kv, &b); });
+        void *s = (void *)current.stream();
+        int st;
+        VQ_WITHOUT_GIL(st, lib.attn_paged(&kv, &b, q.p, q.stride, sm_scale, out, out_stride, ws.p, ws.bytes, s));
+        check(st, "vq_attn_paged");
+        if (args[6] == Py_None) return THPVariable_Wrap(own);
+        Py_INCREF(args[6]);
+        return args[6];
+    });
+}
+
+// (thirteen addresses, VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError, VQKVPagesDev, VQPagePlan)
 PyObject *init(PyObject *, PyObject *args) {
-    unsigned long long a[9];
-    if (!PyArg_ParseTuple(args, "(KKKKKKKKK)OOOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &weight_type, &kv_type, &pack_type, &error_type))
+    unsigned long long a[13];
+    if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKKK)OOOOOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &a[12], &weight_type, &kv_type,
+                          &pack_type, &error_type, &pages_type, &plan_type))
         return nullptr;
-    for (PyObject *o : {weight_type, kv_type, pack_type, error_type}) Py_INCREF(o);
+    for (PyObject *o : {weight_type, kv_type, pack_type, error_type, pages_type, plan_type}) Py_INCREF(o);
     lib.gemv = (decltype(lib.gemv))a[0];
     lib.gemv_workspace = (decltype(lib.gemv_workspace))a[1];
     lib.gemv_batch = (decltype(lib.gemv_batch))a[2];
@@ -384,6 +553,10 @@ PyObject *init(PyObject *, PyObject *args) {
     lib.attn_decode = (decltype(lib.attn_decode))a[6];
     lib.attn_decode_workspace = (decltype(lib.attn_decode_workspace))a[7];
     lib.kv_quantize = (decltype(lib.kv_quantize))a[8];
+    lib.kv_pages_assign = (decltype(lib.kv_pages_assign))a[9];
+    lib.kv_quantize_paged = (decltype(lib.kv_quantize_paged))a[10];
+    lib.attn_paged = (decltype(lib.attn_paged))a[11];
+    lib.attn_paged_workspace = (decltype(lib.attn_paged_workspace))a[12];
     Py_RETURN_NONE;
 }
 
@@ -394,6 +567,9 @@ PyMethodDef methods[] = {
     {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr},
     {"attn_decode", (PyCFunction)(void (*)(void))attn_decode, METH_FASTCALL, nullptr},
     {"kv_quantize", (PyCFunction)(void (*)(void))kv_quantize, METH_FASTCALL, nullptr},
+    {"kv_pages_assign", (PyCFunction)(void (*)(void))kv_pages_assign, METH_FASTCALL, nullptr},
+    {"kv_quantize_paged", (PyCFunction)(void (*)(void))kv_quantize_paged, METH_FASTCALL, nullptr},
+    {"attn_paged", (PyCFunction)(void (*)(void))attn_paged, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -406,12 +582,15 @@ PyMODINIT_FUNC PyInit__marshal() {
         const char *name;
     } names[] = {{&s_N, "N"}, {&s_K, "K"}, {&s_v, "v"}, {&s_code_bits, "code_bits"}, {&s_codes, "codes"}, {&s_codebooks, "codebooks"}, {&s_scale, "scale"},
                  {&s_pack, "pack"}, {&s_hot_entries, "hot_entries"}, {&s_cb_tile, "cb_tile"}, {&s_B, "B"}, {&s_H, "H"}, {&s_D, "D"}, {&s_T, "T"},
-                 {&s_k_codes, "k_codes"}, {&s_v_codes, "v_codes"}, {&s_k_codebooks, "k_codebooks"}, {&s_v_codebooks, "v_codebooks"}, {&s_seq_lens, "seq_lens"}};
+                 {&s_k_codes, "k_codes"}, {&s_v_codes, "v_codes"}, {&s_k_codebooks, "k_codebooks"}, {&s_v_codebooks, "v_codebooks"}, {&s_seq_lens, "seq_lens"},
+                 {&s_page_tokens, "page_tokens"}, {&s_cu_new, "cu_new"}, {&s_slots, "slots"}, {&s_positions, "positions"}, {&s_status, "status"}};
     for (const auto &n : names)
         if (!(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
     PyObject *m = PyModule_Create(&module);
     // binding.py compares this with what it runs under before it calls init
-    PyObject *built_for = m ? Py_BuildValue("(snnn)", VQ_BUILT_FOR, (Py_ssize_t)sizeof(vq_weight_t), (Py_ssize_t)sizeof(vq_kv_t), (Py_ssize_t)sizeof(vq_gemv_pack_t)) : nullptr;
+    PyObject *built_for = m ? Py_BuildValue("(snnnnnn)", VQ_BUILT_FOR, (Py_ssize_t)sizeof(vq_weight_t), (Py_ssize_t)sizeof(vq_kv_t), (Py_ssize_t)sizeof(vq_gemv_pack_t),
+                                            (Py_ssize_t)sizeof(vq_kv_pages_t), (Py_ssize_t)sizeof(vq_page_step_t), (Py_ssize_t)sizeof(vq_paged_batch_t))
+                            : nullptr;
     if (!built_for || PyModule_AddObject(m, "built_for", built_for) != 0) {
         Py_XDECREF(built_for);
         Py_XDECREF(m);

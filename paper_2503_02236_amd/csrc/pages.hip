@@ -1,6 +1,8 @@
 // Pages of a step of continuous batching, built on the GPU: block tables, slot maps and positions from the lengths that requests
 // have and get (vq_kv_pages_assign).  Integer work of a few kilobytes: bound by the latency of a launch and of the
-// dependent trips to memory in it, so one workgroup does all of it, with one lane per request and three scans.
+// dependent trips to memory in it (lengths, free pages, table, slots), so one workgroup does all of it: a lane per request, one scan where
+// everyone is served, pages and tokens dealt out to all lanes by a search in the scan's sums.  Slots of many tokens are a second
+// launch, over the chip.
 #include "vq_common.h"
 
 namespace vq {
@@ -8,6 +10,10 @@ namespace vq {
 namespace {
 
 constexpr int kAssignThreads = 1024, kAssignWaves = kAssignThreads / kWave;
+constexpr int kEndsInLds = 4096;      // requests whose ends a workgroup keeps in LDS
+constexpr int kSlotThreads = 256;
+// Tokens that the one workgroup takes along: two a lane.
+constexpr int kFewTokens = 2 * kAssignThreads;
 
 struct AssignArgs {
     vq_page_step_t p;
@@ -15,17 +21,17 @@ struct AssignArgs {
 };
 
 // Inclusive sum over the workgroup's threads and the sum of all of them (xs: kAssignWaves values of LDS).
-__device__ __forceinline__ long long scan(long long x, long long *xs, long long *total) {
+__device__ __forceinline__ unsigned long long scan(unsigned long long x, unsigned long long *xs, unsigned long long *total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const long long y = __shfl_up(x, d, 64);
+        const unsigned long long y = __shfl_up(x, d, 64);
         if (lane >= d) x += y;
     }
     __syncthreads();   // (xs may still be read from the last scan)
     if (lane == 63) xs[wave] = x;
     __syncthreads();
-    long long before = 0, all = 0;
+    unsigned long long before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < kAssignWaves; ++w) {
         if (w < wave) before += xs[w];
@@ -37,88 +43,150 @@ __device__ __forceinline__ long long scan(long long x, long long *xs, long long 
 
 __device__ __forceinline__ long long pages_of(long long tokens, int log_ps) { return (tokens + (1ll << log_ps) - 1) >> log_ps; }
 
-__global__ __launch_bounds__(kAssignThreads) void kv_pages_assign_kernel(AssignArgs a) {
-    __shared__ long long xs[kAssignWaves];
+// The first of n ascending ends that lies behind t.
+__device__ __forceinline__ int owner_of(const int *ends, int n, int t) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ends[mid] > t) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Things 0 .. n - 1 of a chunk of requests, number j of request l where upto (the requests' sums) says so, dealt out to all lanes:
+// load(l, j) and then store(i, l, j, what was loaded), four of a lane at once (no load here reads what a store writes).
+template <typename Load, typename Store>
+__device__ __forceinline__ void deal(int n, const int *upto, Load load, Store store) {
+    for (int i0 = threadIdx.x; i0 < n; i0 += 4 * kAssignThreads) {
+        int l[4], j[4], x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {   // (past the end: the last one once more, not stored)
+            const int i = min(i0 + k * kAssignThreads, n - 1);
+            l[k] = owner_of(upto, kAssignThreads, i);
+            j[k] = i - (l[k] ? upto[l[k] - 1] : 0);
+            x[k] = load(l[k], j[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i0 + k * kAssignThreads < n) store(i0 + k * kAssignThreads, l[k], j[k], x[k]);
+    }
+}
+
+// Slot and position of new token t of `tokens`; ends: cu_new + 1.
+__device__ __forceinline__ void write_slot(const AssignArgs &a, const int *ends, int tokens, int t) {
     const vq_page_step_t &p = a.p;
-    const int tid = threadIdx.x, lane = tid & 63;
+    int slot = -1, pos = -1;
+    if (t < tokens) {
+        const int b = owner_of(ends, p.B, t);
+        pos = p.seq_lens[b] - (ends[b] - t);
+        const int page = p.block_table[(size_t)b * p.max_pages + (pos >> a.log_ps)];
+        if ((unsigned)page < (unsigned)p.n_pages) slot = (page << a.log_ps) + (pos & ((1 << a.log_ps) - 1));
+    }
+    p.slots[t] = slot;
+    if (p.positions) p.positions[t] = pos;
+}
+
+__global__ __launch_bounds__(kAssignThreads) void kv_pages_assign_kernel(AssignArgs a) {
+    __shared__ unsigned long long xs[kAssignWaves];
+    __shared__ int upto[kAssignThreads], base[kAssignThreads], ends[kEndsInLds];
+    const vq_page_step_t &p = a.p;
+    const int tid = threadIdx.x;
     const long long row = (long long)p.max_pages << a.log_ps;   // tokens of a row of the table
     const int n_free = min(max(p.n_free[0], 0), p.n_pages);
     auto len_of = [&](int b) { return (long long)min((long long)max(p.lens[b], 0), row); };
-    // 1. pages of the requests that have ended
-    long long freed = 0, total;
+    unsigned long long total;
+    // 1. pages of the requests that have ended (where any has)
+    long long freed = 0;
     for (int b0 = 0; b0 < p.B; b0 += kAssignThreads) {
         const int b = b0 + tid;
         const bool gone = b < p.B && p.new_lens[b] < 0;
+        if (!__syncthreads_or(gone)) continue;
         const int count = gone ? (int)pages_of(len_of(b), a.log_ps) : 0;
-        const long long at = n_free + freed + scan(count, xs, &total) - count;
-        for (unsigned long long left = __ballot(count > 0); left; left &= left - 1) {   // a wavefront copies one request's pages at a time
-            const int l = __ffsll((long long)left) - 1, c = __shfl(count, l, 64);
-            const long long to = __shfl(at, l, 64);
-            const int *from = p.block_table + (size_t)__shfl(b, l, 64) * p.max_pages;
-            for (int j = lane; j < c; j += 64)
-                if (to + j < p.n_pages) p.free_pages[to + j] = from[j];
-        }
+        upto[tid] = (int)scan(count, xs, &total);
+        __syncthreads();
+        deal((int)total, upto, [&](int l, int j) { return p.block_table[(size_t)(b0 + l) * p.max_pages + j]; },
+             [&](int i, int, int, int page) {
+                 if (n_free + freed + i < p.n_pages) p.free_pages[n_free + freed + i] = page;
+             });
         freed += total;
+        __syncthreads();
     }
     const long long pool = min(n_free + freed, (long long)p.n_pages);
     __syncthreads();
     // 2. new tokens
-    long long asked = 0, needed = 0, served = 0, tokens = 0;   // asked and needed so far, pages and tokens given so far
+    unsigned long long asked = 0, needed = 0, served = 0, tokens = 0;   // tokens asked for and pages needed so far, pages and tokens given so far
     for (int b0 = 0; b0 < p.B; b0 += kAssignThreads) {
         const int b = b0 + tid;
         const bool live = b < p.B;
         const int n = live ? p.new_lens[b] : 0;
-        const long long len = live && n >= 0 ? len_of(b) : 0;
-        bool fits = n <= 0 || len + n <= row;
-        const long long ask = fits && n > 0 ? n : 0;
-        const long long ask_to = asked + scan(ask, xs, &total);
-        asked += total;
-        fits = fits && (ask == 0 || ask_to <= p.n_tokens);
-        const long long have = pages_of(len, a.log_ps), want = fits && n > 0 ? pages_of(len + n, a.log_ps) - have : 0;
-        const long long want_to = needed + scan(want, xs, &total);
-        needed += total;
-        fits = fits && (want == 0 || want_to <= pool);
-        const int need = fits ? (int)want : 0, give = fits && n > 0 ? n : 0;
-        const long long give_to = tokens + scan(give, xs, &total);
-        tokens += total;
-        scan(need, xs, &total);
-        served += total;
+        const long long len = live && n >= 0 ? len_of(b) : 0, have = pages_of(len, a.log_ps);
+        const bool room = n <= 0 || len + n <= row;
+        const unsigned long long ask = room && n > 0 ? n : 0, want = ask ? pages_of(len + n, a.log_ps) - have : 0;
+        // Both sums in one: 1024 requests ask for less than 2^41 tokens and want fewer pages than are in the table, 2^31; the tokens are counted
+        // up to 2^21 each, more than a step takes.
+        const unsigned long long both = scan((want << 32) | min(ask, 1ull << 21), xs, &total);
+        unsigned long long ask_to = asked + (both & 0xFFFFFFFFull), want_to = needed + (both >> 32);
+        bool fits = room;
+        unsigned long long give = ask, need = want, give_to = ask_to - asked, need_to = want_to - needed;
+        if (asked + (total & 0xFFFFFFFFull) <= (unsigned long long)p.n_tokens && needed + (total >> 32) <= (unsigned long long)pool) {   // everyone is served
+            asked += total & 0xFFFFFFFFull;
+            needed += total >> 32;
+        } else {
+            unsigned long long t;
+            fits = fits && (ask == 0 || ask_to <= (unsigned long long)p.n_tokens);
+            asked += total & 0xFFFFFFFFull;
+            need = fits ? want : 0;
+            want_to = needed + scan(need, xs, &t);
+            needed += t;
+            fits = fits && (need == 0 || want_to <= (unsigned long long)pool);
+            need = fits ? need : 0;
+            give = fits ? ask : 0;
+            const unsigned long long given = scan((need << 32) | give, xs, &total);
+            give_to = given & 0xFFFFFFFFull;
+            need_to = given >> 32;
+        }
         if (live) {
+            const int end = (int)(tokens + give_to);
             p.status[b] = fits ? 0 : 1;
             p.seq_lens[b] = (int)(len + give);
-            p.cu_new[b + 1] = (int)give_to;
+            p.cu_new[b + 1] = end;
+            if (b < kEndsInLds) ends[b] = end;
         }
-        // (requests are served in order, so those served before b needed want_to - want pages)
-        const long long first = pool - 1 - (want_to - want);
-        for (unsigned long long left = __ballot(need > 0); left; left &= left - 1) {
-            const int l = __ffsll((long long)left) - 1, c = __shfl(need, l, 64);
-            const long long from = __shfl(first, l, 64);
-            int *to = p.block_table + (size_t)__shfl(b, l, 64) * p.max_pages + __shfl((int)have, l, 64);
-            for (int j = lane; j < c; j += 64) to[j] = p.free_pages[from - j];
-        }
+        // (requests are served in order: what those before this chunk got is what they needed, up to the first that was refused for want of pages, behind
+        // whom nobody gets any)
+        upto[tid] = (int)need_to;
+        base[tid] = (int)have;
+        __syncthreads();
+        const int pages = (int)(total >> 32);
+        deal(pages, upto, [&](int l, int j) { return p.free_pages[pool - 1 - (long long)served - ((l ? upto[l - 1] : 0) + j)]; },
+             [&](int, int l, int j, int page) { p.block_table[(size_t)(b0 + l) * p.max_pages + base[l] + j] = page; });
+        served += pages;
+        tokens += total & 0xFFFFFFFFull;
+        __syncthreads();
     }
     if (tid == 0) {
         p.cu_new[0] = 0;
-        p.n_free_out[0] = (int)(pool - served);
+        p.n_free_out[0] = (int)(pool - (long long)served);
     }
-    __syncthreads();
     // 3. slots and positions
-    for (int t = tid; t < p.n_tokens; t += kAssignThreads) {
-        int slot = -1, pos = -1;
-        if (t < tokens) {
-            int lo = 0, hi = p.B - 1;   // the request: the first whose end lies behind t
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (p.cu_new[mid + 1] > t) hi = mid;
-                else lo = mid + 1;
-            }
-            pos = p.seq_lens[lo] - (p.cu_new[lo + 1] - t);
-            const int page = p.block_table[(size_t)lo * p.max_pages + (pos >> a.log_ps)];
-            if ((unsigned)page < (unsigned)p.n_pages) slot = (page << a.log_ps) + (pos & ((1 << a.log_ps) - 1));
-        }
-        p.slots[t] = slot;
-        if (p.positions) p.positions[t] = pos;
+    if (p.n_tokens > kFewTokens) return;
+    const int *e = p.B <= kEndsInLds ? ends : p.cu_new + 1;
+    for (int t = tid; t < p.n_tokens; t += kAssignThreads) write_slot(a, e, (int)tokens, t);
+}
+
+__global__ __launch_bounds__(kSlotThreads) void kv_pages_slots_kernel(AssignArgs a) {
+    __shared__ int ends[kEndsInLds];
+    const vq_page_step_t &p = a.p;
+    const int tokens = p.cu_new[p.B];
+    const int *e = p.cu_new + 1;
+    if (p.B <= kEndsInLds) {
+        for (int b = threadIdx.x; b < p.B; b += kSlotThreads) ends[b] = e[b];
+        __syncthreads();
+        e = ends;
     }
+    const int t = blockIdx.x * kSlotThreads + threadIdx.x;
+    if (t < p.n_tokens) write_slot(a, e, tokens, t);
 }
 
 }  // namespace
@@ -128,6 +196,7 @@ int launch_kv_pages_assign(const vq_page_step_t *step, hipStream_t s) {
     a.p = *step;
     a.log_ps = __builtin_ctz(step->page_tokens);
     kv_pages_assign_kernel<<<1, kAssignThreads, 0, s>>>(a);
+    if (step->n_tokens > kFewTokens) kv_pages_slots_kernel<<<(step->n_tokens + kSlotThreads - 1) / kSlotThreads, kSlotThreads, 0, s>>>(a);
     return launch_status();
 }
 

@@ -742,3 +742,40 @@ def test_one_request_in_pages_is_the_contiguous_cache(gpu_device):
     want = vq.vq_attn_decode(kd, t(case.q), case.sm_scale).float()
     _, bound = case.attend()
     assert bool(((got - want).abs() <= 2 * torch.from_numpy(bound).to(gpu_device)).all())
+
+
+@gpu
+def test_native_marshalling_does_what_ctypes_does(gpu_device, monkeypatch):
+    """The three calls through the native part of the binding and without it: the same results, and the same errors for what does not fit."""
+    from paper_2503_02236_amd import binding
+    native = binding._marshal
+    assert native is not None, "the native part of the binding is not built"
+    case = Case([(300, 20), (40, 1)], group=2, seed=31, window=90, softcap=9.0, slopes=[0.01, 0.0, 0.3, 0.02], prefix=[5, 0])
+    kv, q, table, cu, seq, mods = case.dev(gpu_device, "strided")
+    results = []
+    for which in (native, None):
+        monkeypatch.setattr(binding, "_marshal", which)
+        out = torch.zeros(q.shape, dtype=torch.float16, device=gpu_device)
+        assert vq.vq_attn_paged(kv, q, case.sm_scale, table, cu, seq, out=out, **mods) is out
+        fresh = vq.vq_attn_paged(kv, q, case.sm_scale, table, cu, seq, **mods)
+        codes = vq.VQKVPagesDev(kv.H, kv.D, kv.v, kv.page_tokens, kv.k_codes.clone(), kv.v_codes.clone(), kv.k_codebooks, kv.v_codebooks)
+        vq.vq_kv_quantize_paged(codes, q[:, :2], q[:, 2:], torch.arange(21, dtype=torch.int32, device=gpu_device) + 3)
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=gpu_device)  # noqa: E731
+        lens, new, tab, free, n_free = i32([3, 40]), i32([20, -1]), i32([[5, -1, -1], [1, 2, 3]]), i32([0, 4, -9, -9, -9, -9]), i32([2])
+        plan = vq.VQPagePlan(2, 30, gpu_device)
+        assert vq.vq_kv_pages_assign(new, lens, tab, free, n_free, 16, plan=plan) is plan
+        results.append([out, fresh, codes.k_codes, codes.v_codes, tab, free, n_free, plan.cu_new, plan.seq_lens, plan.slots, plan.positions, plan.status])
+        for bad in (dict(slopes=torch.zeros(3, device=gpu_device)), dict(prefix_lens=cu), dict(out=out[:, :3]), dict(softcap=-1.0), dict(window=-4)):
+            with pytest.raises((ValueError, TypeError, vq.VQError)):
+                vq.vq_attn_paged(kv, q, case.sm_scale, table, cu, seq, **bad)
+        with pytest.raises(ValueError):
+            vq.vq_kv_quantize_paged(codes, q[:, :2], q[:, 2:], torch.arange(20, dtype=torch.int32, device=gpu_device))
+        with pytest.raises(ValueError):
+            vq.vq_kv_quantize_paged(codes, q[:, :3], q[:, :3], torch.arange(21, dtype=torch.int32, device=gpu_device))
+        with pytest.raises(TypeError):
+            vq.vq_kv_pages_assign(new.long(), lens, tab, free, n_free, 16, plan=plan)
+        with pytest.raises(vq.VQError):
+            vq.vq_kv_pages_assign(new, lens, tab, free, n_free, 15, plan=plan)
+        torch.cuda.synchronize()
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
