@@ -54,22 +54,30 @@ __device__ __forceinline__ int owner_of(const int *ends, int n, int t) {
     return lo;
 }
 
-// Things 0 .. n - 1 of a chunk of requests, number j of request l where upto (the requests' sums) says so, dealt out to all lanes:
-// load(l, j) and then store(i, l, j, what was loaded), four of a lane at once (no load here reads what a store writes).
+// Things 0 .. n - 1 of a chunk of requests, number j of request l where upto (the requests' sums) says so, dealt out to the lanes, a
+// wavefront a run of them: load(l, j) and then store(i, l, j, what was loaded), eight of a lane's at once (no load here reads what a store
+// writes).  A lane looks for the owner of its first thing and for another one where the run leaves that: the ten dependent reads of LDS of a
+// search take longer than a trip to L2.
 template <typename Load, typename Store>
 __device__ __forceinline__ void deal(int n, const int *upto, Load load, Store store) {
-    for (int i0 = threadIdx.x; i0 < n; i0 += 4 * kAssignThreads) {
-        int l[4], j[4], x[4];
+    const int per = (n + kAssignThreads - 1) / kAssignThreads, from = (int)(threadIdx.x >> 6) * 64 * per;
+    const int end = min(from + 64 * per, n);
+    int i = from + (int)(threadIdx.x & 63);
+    if (i >= end) return;
+    int at = owner_of(upto, kAssignThreads, i);
+    for (; i < end; i += 8 * 64) {
+        int l[8], j[8], x[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {   // (past the end: the last one once more, not stored)
-            const int i = min(i0 + k * kAssignThreads, n - 1);
-            l[k] = owner_of(upto, kAssignThreads, i);
-            j[k] = i - (l[k] ? upto[l[k] - 1] : 0);
-            x[k] = load(l[k], j[k]);
-        }
+        for (int k = 0; k < 8; ++k)
+            if (i + 64 * k < end) {
+                if (upto[at] <= i + 64 * k) at += 1 + owner_of(upto + at + 1, kAssignThreads - at - 1, i + 64 * k);
+                l[k] = at;
+                j[k] = i + 64 * k - (at ? upto[at - 1] : 0);
+                x[k] = load(at, j[k]);
+            }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (i0 + k * kAssignThreads < n) store(i0 + k * kAssignThreads, l[k], j[k], x[k]);
+        for (int k = 0; k < 8; ++k)
+            if (i + 64 * k < end) store(i + 64 * k, l[k], j[k], x[k]);
     }
 }
 
