@@ -107,6 +107,10 @@ __device__ __forceinline__ Request request_of(const PagedArgs &a, int b) {
     return r;
 }
 
+__device__ __forceinline__ long long shfl_ll(long long v, int from) {
+    return ((long long)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, from);
+}
+
 // The share of worker w: rounds [u0, u1) of the head's, the first of them round x of request b.  False: none.  All threads of the
 // workgroup call it; xs: LDS, threads / 64 + 2 values.
 struct Share {
@@ -117,6 +121,29 @@ template <int THREADS>
 __device__ __forceinline__ bool find_share(const PagedArgs &a, int w, long long *xs, Share *out) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int NW = THREADS / 64;
+    auto share_of = [&](long long total) {
+        out->share = max((total + a.workers - 1) / a.workers, (long long)a.min_share);
+        out->u0 = w * out->share;
+        out->u1 = min(out->u0 + out->share, total);
+        return out->u0 < total;
+    };
+    if (a.B <= 64) {   // every wavefront for itself
+        long long own = 0;
+        if (lane < a.B) {
+            const Request r = request_of(a, lane);
+            own = (long long)r.items * r.C;
+        }
+        long long upto = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long y = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += y;
+        }
+        if (!share_of(shfl_ll(upto, 63))) return false;
+        out->b = __ffsll((long long)__ballot(out->u0 < upto)) - 1;
+        out->x = out->u0 - shfl_ll(upto - own, out->b);
+        return true;
+    }
     long long mine = 0, total = 0, own = 0;
     for (int b = tid; b < a.B; b += THREADS) {
         const Request r = request_of(a, b);
@@ -138,10 +165,7 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, int w, long long 
         total += xs[i];
     }
     incl += before;
-    out->share = max((total + a.workers - 1) / a.workers, (long long)a.min_share);
-    out->u0 = w * out->share;
-    out->u1 = min(out->u0 + out->share, total);
-    if (out->u0 >= total) return false;
+    if (!share_of(total)) return false;
     __syncthreads();
     if (a.B <= THREADS) {
         if (incl - mine <= out->u0 && out->u0 < incl) {
@@ -202,9 +226,6 @@ __device__ __forceinline__ Piece uniform_piece(const Piece &p) {
     for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_readfirstlane(t[i]);
     __builtin_memcpy(&u, t, sizeof(Piece));
     return u;
-}
-__device__ __forceinline__ long long shfl_ll(long long v, int from) {
-    return ((long long)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, from);
 }
 
 // The next pieces of a share, 64 at most: from round *x of request *b on, *left rounds; all three step behind them.  A lane makes a piece:
@@ -347,72 +368,62 @@ __device__ __forceinline__ unsigned row_address(uint32_t w, unsigned lane_const)
     return __builtin_amdgcn_perm(w, lane_const, 0x0c020000u | ((4u + B) << 8));
 }
 
-// One side's codebooks of a head (cb) to LDS, for gathers of whole entries: every entry 256 / (2 v) times in a row of 256 bytes, or a
-// table per sub-vector.  Rows of entries that do not exist are zero.
-template <int D, int V, bool COPIES>
-__device__ __forceinline__ void stage_entries(const PagedArgs &a, const unsigned char *cb, unsigned char *to, int tid) {
-    constexpr int ES = 2 * V, P = D / V;
-    typedef typename Raw<ES>::type entry_t;
-    const entry_t none = {};
-    if constexpr (COPIES) {
-        constexpr int N = 256 * 16 / kThreads;      // units of 16 bytes
-        entry_t e[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) e[i] = global_read<ES>(cb + (unsigned)(min((tid + i * kThreads) >> 4, a.E - 1) * ES));
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            entry_t r[16 / ES];
-#pragma unroll
-            for (int k = 0; k < 16 / ES; ++k) r[k] = ((tid + i * kThreads) >> 4) < a.E ? e[i] : none;
-            uint4 u;
-            __builtin_memcpy(&u, r, 16);
-            reinterpret_cast<uint4 *>(to)[tid + i * kThreads] = u;
-        }
-    } else {
-        constexpr int N = P * 256 / kThreads;
-        entry_t e[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = tid + i * kThreads, row = u & 255, p = u >> 8;
-            e[i] = global_read<ES>(cb + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES));
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) reinterpret_cast<entry_t *>(to)[tid + i * kThreads] = ((tid + i * kThreads) & 255) < a.E ? e[i] : none;
-    }
-}
-// The same for gathers by channel position (v = 2): row e holds entry e for all 32 positions of the operand.
-template <int D, int V, bool COPIES>
-__device__ __forceinline__ void stage_positions(const PagedArgs &a, const unsigned char *cb, unsigned char *to, int tid) {
-    constexpr int ES = 2 * V;
-    constexpr int CH = D / 32, US = 2 * (V < CH ? V : CH), UNITS = 2 * D / US;   // parts of an entry that one lane takes
-    constexpr int N = 256 * UNITS / kThreads;
+// One side's codebooks of a head (cb) for LDS: load() requests them, store() writes them.  By entry: every entry 256 / (2 v) times in a row of
+// 256 bytes, or a table per sub-vector.  By position (v = 2, values): row e holds entry e for all 32 positions of the operand.  Rows of
+// entries that do not exist are zero.
+template <int D, int V, bool COPIES, bool POSITIONS>
+struct Tables {
+    static constexpr int ES = 2 * V, P = D / V, CH = D / 32;
+    static constexpr int US = POSITIONS ? 2 * (V < CH ? V : CH) : ES;      // bytes of a unit of memory
+    static constexpr int UNITS = 2 * D / US;                               // POSITIONS: units of a row
+    static constexpr int N = (POSITIONS ? 256 * UNITS : COPIES ? 256 * 16 : P * 256) / kThreads;
     typedef typename Raw<US>::type unit_t;
-    const unit_t zero = {};
-    unit_t e[N];
-    auto place = [&](int i, int *row, int *unit) {
-        const int u = tid + i * kThreads;
-        if (COPIES) {   // neighbours read one entry
-            *row = u / UNITS;
-            *unit = u % UNITS;
-        } else {        // eight entries of eight positions: 64-byte pieces from memory, eight columns of LDS
-            *row = (u >> 3) / UNITS * 8 + (u & 7);
-            *unit = (u >> 3) % UNITS;
+    unit_t u[N];
+
+    static __device__ __forceinline__ void place(int at, int *row, int *unit) {
+        if (!POSITIONS) {
+            *row = COPIES ? at >> 4 : at & 255;
+            *unit = COPIES ? 0 : at >> 8;
+        } else if (COPIES) {   // neighbours read one entry
+            *row = at / UNITS;
+            *unit = at % UNITS;
+        } else {               // eight entries of eight positions: 64-byte pieces from memory, eight columns of LDS
+            *row = (at >> 3) / UNITS * 8 + (at & 7);
+            *unit = (at >> 3) % UNITS;
         }
-    };
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        int row, unit;
-        place(i, &row, &unit);
-        const int ch = unit * (US / 2), p = ch / V;
-        e[i] = global_read<US>(cb + (unsigned)(((p >> a.pg_shift) * a.E + min(row, a.E - 1)) * ES + (ch % V) * 2));
     }
+    __device__ __forceinline__ void load(const PagedArgs &a, const unsigned char *cb, int tid) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        int row, unit;
-        place(i, &row, &unit);
-        *reinterpret_cast<unit_t *>(to + row * 256 + unit * US) = row < a.E ? e[i] : zero;
+        for (int i = 0; i < N; ++i) {
+            int row, unit;
+            place(tid + i * kThreads, &row, &unit);
+            const int ch = POSITIONS ? unit * (US / 2) : unit * V, p = COPIES ? 0 : (ch / V) >> a.pg_shift;
+            u[i] = global_read<US>(cb + (unsigned)((p * a.E + min(row, a.E - 1)) * ES + (POSITIONS ? ch % V * 2 : 0)));
+        }
     }
-}
+    __device__ __forceinline__ void store(const PagedArgs &a, unsigned char *to, int tid) const {
+        const unit_t none = {};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = tid + i * kThreads;
+            int row, unit;
+            place(at, &row, &unit);
+            const unit_t x = row < a.E ? u[i] : none;
+            if (POSITIONS) {
+                *reinterpret_cast<unit_t *>(to + row * 256 + unit * US) = x;
+            } else if (COPIES) {
+                unit_t r[16 / US];
+#pragma unroll
+                for (int k = 0; k < 16 / US; ++k) r[k] = x;
+                uint4 q;
+                __builtin_memcpy(&q, r, 16);
+                reinterpret_cast<uint4 *>(to)[at] = q;
+            } else {
+                reinterpret_cast<unit_t *>(to)[at] = x;
+            }
+        }
+    }
+};
 
 template <int D, int V, bool COPIES, bool MODS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_paged_kernel(PagedArgs a) {
@@ -434,8 +445,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int nwg = gridDim.x, id = (nwg & 7) == 0 ? (int)(blockIdx.x & 7) * (nwg >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
     const int h = id / a.workers, w = id - h * a.workers;
 
+    // The codebooks first (they arrive while the share is looked for), the codes next (they arrive while the codebooks are written).
+    Tables<D, V, COPIES, false> k_books;
+    Tables<D, V, COPIES, !TR> v_books;
+    const size_t books = (size_t)h * a.G * a.E * ES;
+    k_books.load(a, reinterpret_cast<const unsigned char *>(a.k_cb) + books, tid);
+    v_books.load(a, reinterpret_cast<const unsigned char *>(a.v_cb) + books, tid);
     Share sh;
     if (!find_share<kThreads>(a, w, reinterpret_cast<long long *>(smem + kScanOff), &sh)) return;
+    k_books.store(a, smem, tid);
+    v_books.store(a, smem + kSide, tid);
 
     const int ps_mask = (1 << a.log_ps) - 1;
     // TR: the position block of a lane's V codes and its keys among the 16 of its half
@@ -455,7 +474,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
     long long left = sh.u1 - sh.u0, x = sh.x;
     int b = sh.b;
-    bool staged = false;
     while (left > 0) {
         int rounds_in_list;
         __syncthreads();   // (the list before is done with)
@@ -508,16 +526,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         };
 #pragma unroll
         for (int u = 0; u < NB; ++u) fetch(u, ring[u]);
-        if (!staged) {   // (while the first codes are on their way)
-            int t = tid;
-            asm volatile("" : "+v"(t));   // (or its addresses are formed before the loop, and lie in scratch)
-            const size_t cb = (size_t)h * a.G * a.E * ES;
-            stage_entries<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.k_cb) + cb, smem, t);
-            if constexpr (TR) stage_entries<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.v_cb) + cb, smem + kSide, t);
-            else stage_positions<D, V, COPIES>(a, reinterpret_cast<const unsigned char *>(a.v_cb) + cb, smem + kSide, t);
-            __syncthreads();
-            staged = true;
-        }
         // K entries of a tile as operands: one gather
         V16 kop[NC];
         auto gather_k = [&](const Codes &codes, int at) {
