@@ -327,7 +327,7 @@ __device__ __forceinline__ int list_pieces(const PagedArgs &a, int *b, long long
 
 // Sums of cut blocks: two per worker (the block that its share begins inside, the one that it ends inside), [rows][D] and [rows][2].
 __device__ __forceinline__ size_t part_of(const PagedArgs &a, int h, int w, int which) { return ((size_t)h * a.workers + w) * 2 + which; }
-__device__ __forceinline__ int part_rows(const PagedArgs &a) { return (kWaves * 32) >> a.min_log_ways; }
+__host__ __device__ __forceinline__ int part_rows(const PagedArgs &a) { return (kWaves * 32) >> a.min_log_ways; }
 template <int D>
 __device__ __forceinline__ float *part_sums(const PagedArgs &a, size_t part) { return a.ws + part * part_rows(a) * D; }
 template <int D>
@@ -609,12 +609,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         }
                     }
                 }
-                if constexpr (MODS) {
+                if constexpr (MODS) {   // (two uniform branches: a choice per score would compute both sides)
+                    if (a.cap_out > 0.f) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float z = a.cap_out > 0.f ? a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f) : s[e] * a.scale2;
-                        const int key = t0 + 16 * lh + 4 * (e & 3) + (e >> 2);
-                        s[e] = z - slope2 * fabsf((float)(pos - key));
+                        for (int e = 0; e < 16; ++e) s[e] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[e] *= scale2;
+                    }
+                    if (a.slopes) {
+                        const float back = (float)(pos - t0 - 16 * lh);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[e] -= slope2 * fabsf(back - (float)(4 * (e & 3) + (e >> 2)));
                     }
                 }
                 if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
@@ -844,6 +850,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
+constexpr int kMergeRows = 32;   // of a workgroup
 // Joins the sums of the block that worker w's share begins inside, if no worker before it began there too.
 template <int D>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedArgs a) {
@@ -861,27 +868,47 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedArgs a) {
         off = nl;
         rounds = block_rounds(a, r, k);
     }
-    if (from <= off || from >= off + rounds || from - sh.share > off) return;
+    if ((int)blockIdx.z * kMergeRows >= block_rows(r) || from <= off || from >= off + rounds || from - sh.share > off) return;
     // pieces: the end of worker w - 1's share, then the beginnings of w's and of those behind it that begin inside the block
     const long long end = sh.u0 - from + min(off + rounds, r.C);
     const int pieces = 1 + (int)((end - sh.u0 + sh.share - 1) / sh.share);
     const int row0 = j * block_rows(r), rows = min(block_rows(r), r.rows - row0);
     constexpr int PER = D / 8;   // threads of a row
-    for (int t = tid; t < rows * PER; t += 256) {
-        const int lr = t / PER, ch = (t - lr * PER) * 8, row = row0 + lr;
-        float M = -FLT_MAX, L = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int t = tid; t < kMergeRows * PER; t += 256) {
+        const int lr = blockIdx.z * kMergeRows + t / PER, ch = t % PER * 8, row = row0 + lr;
+        if (lr >= rows) break;
+        // (four pieces at a time are requested at once: each is a trip to memory, or two)
+        constexpr int N = 4;
         auto part = [&](int p) { return part_of(a, h, w - 1 + p, p == 0 ? 1 : 0); };
-        for (int p = 0; p < pieces; ++p) M = fmaxf(M, part_stats<D>(a, part(p))[lr * 2]);
-        for (int p = 0; p < pieces; ++p) {
-            const float *st = part_stats<D>(a, part(p)) + lr * 2;
-            const float f = __builtin_amdgcn_exp2f(st[0] - M);
-            L += st[1] * f;
-            const float4_t *y = reinterpret_cast<const float4_t *>(part_sums<D>(a, part(p)) + (size_t)lr * D + ch);
-            const float4_t y0 = y[0], y1 = y[1];
+        float M = -FLT_MAX, L = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < pieces; p0 += N) {
+            float m[N], l[N];
+            float4_t y[N][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] += y0[e] * f;
-                x[4 + e] += y1[e] * f;
+            for (int p = 0; p < N; ++p) {   // (past the end: the last one once more, without weight)
+                const size_t from = part(min(p0 + p, pieces - 1));
+                const float *st = part_stats<D>(a, from) + lr * 2;
+                m[p] = st[0];
+                l[p] = st[1];
+                const float4_t *sums = reinterpret_cast<const float4_t *>(part_sums<D>(a, from) + (size_t)lr * D + ch);
+                y[p][0] = sums[0];
+                y[p][1] = sums[1];
+            }
+            float top = M;
+#pragma unroll
+            for (int p = 0; p < N; ++p) top = fmaxf(top, m[p]);
+            const float keep = __builtin_amdgcn_exp2f(M - top);
+            M = top;
+            L *= keep;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= keep;
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+                if (p0 + p >= pieces) break;
+                const float f = __builtin_amdgcn_exp2f(m[p] - M);
+                L += l[p] * f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += y[p][e / 4][e % 4] * f;
             }
         }
         const float inv = L == 0.f ? 0.f : 1.f / L;
@@ -913,7 +940,7 @@ int run_paged(const PagedArgs &a, hipStream_t s) {
     static KernelSetup setup;
     if (int st = kernel_setup(reinterpret_cast<const void *>(&attn_paged_kernel<D, V, COPIES, MODS>), kLds, true, setup)) return st;
     attn_paged_kernel<D, V, COPIES, MODS><<<a.H * a.workers, kThreads, kLds, s>>>(a);
-    if (a.cut) attn_paged_merge_kernel<D><<<dim3(a.workers - 1, a.H), 256, 0, s>>>(a);
+    if (a.cut) attn_paged_merge_kernel<D><<<dim3(a.workers - 1, a.H, part_rows(a) / kMergeRows), 256, 0, s>>>(a);
     return launch_status();
 }
 template <int D, int V>
