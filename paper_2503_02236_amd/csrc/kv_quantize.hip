@@ -610,7 +610,10 @@ int kvq_share(long bh, int ranges, int items) {
 // 8 groups of 64, B16, one token 8.6 / 4.0 / 6.7; 16 entries, v = 4, B64, 4 tokens 73 / 7.2 / 11.1, B2, 2048 tokens 1052 / 51 / 43.
 // Workgroups that share a chain are in each other's way: it takes up to 1.7 times what its part of the items would, and longer the more
 // instructions there are (without that, 104 sequence-heads, 15 tokens, 64 groups of 128, v = 2 came to the scan, 33.0 / - / 24.5).
-int kvq_choice(int bh, int P, int v, int E, int G, int n_new) {
+// scan_tokens: the new tokens are those of many requests (pages), so a workgroup of the scan may take fewer than sixteen of them; how many it does
+// take.  One head's sixteen are a chain that few heads do not hide: 8 heads, 32 groups, 16 tokens 14.0 us by the matrix cores (the choice with sixteen), 5.7 with
+// one token a workgroup, 64 tokens 14.5 / 10.1; 32 heads, 64 groups of v = 2, 16 tokens 24.5 / 13.3, 64 tokens 25.4 / 42.7.
+int kvq_choice(int bh, int P, int v, int E, int G, int n_new, int *scan_tokens = nullptr) {
     const double kInst = 1.63e-6;
     double best = 1e300;
     int pick = kKvqScan;
@@ -622,12 +625,14 @@ int kvq_choice(int bh, int P, int v, int E, int G, int n_new) {
         }
     };
     const double sides = 2.0 * bh;
-    {   // a wavefront takes one item after the other
-        const int tokens = std::min(n_new, kQuantScanTokens), items = tokens * P, ranges = ceil_div(n_new, tokens), share = kvq_share(bh, ranges, items);
+    for (int most = kQuantScanTokens; most >= (scan_tokens ? 1 : kQuantScanTokens); most /= 2) {   // a wavefront takes one item after the other
+        const double before = best;
+        const int tokens = std::min(n_new, most), items = tokens * P, ranges = ceil_div(n_new, tokens), share = kvq_share(bh, ranges, items);
         const double item = 0.33 + 0.045 * v, inst = items * (52.0 + 9 * v);
         double chain = ceil_div(items, 8) * item;
         if (share > 1) chain = std::min(chain, 1.6 * ceil_div(items, 8 * share) * item + 0.5 * sides * ranges * inst * kInst);
         consider(kKvqScan, chain, sides * ranges, 0.0022 * share, inst);
+        if (scan_tokens && best < before) *scan_tokens = tokens;
     }
     if (G * E * v * 2 <= kQuantLaneBytes) {
         const int tokens = std::min(n_new, kQuantLaneTokens), items = tokens * P, log_lanes = kvq_log_lanes(items);
@@ -720,10 +725,11 @@ int run_kvq_lane(KvQuantArgs &a, int bh, hipStream_t s) {
 
 template <int V, bool PAGED>
 int run_kvq(KvQuantArgs &a, int bh, hipStream_t s) {
-    const int kernel = kvq_choice(bh, a.P, V, a.E, a.G, a.n_new);
+    int scan_tokens = kQuantScanTokens;
+    const int kernel = kvq_choice(bh, a.P, V, a.E, a.G, a.n_new, PAGED ? &scan_tokens : nullptr);
     if (kernel == kKvqLane) return run_kvq_lane<V, PAGED>(a, bh, s);
     if (kernel == kKvqScan) {
-        a.tokens = std::min(a.n_new, kQuantScanTokens);
+        a.tokens = std::min(a.n_new, scan_tokens);
         const int ranges = ceil_div(a.n_new, a.tokens);
         a.share = kvq_share(bh, ranges, a.tokens * a.P);
         if (a.share > 1)
