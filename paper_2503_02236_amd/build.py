@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libvqmi.so")
 MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # (another Python does not load it)
-SOURCES = ["api.hip", "dequant.hip", "gemv.hip", "gemv_packed.hip", "gemv_mfma.hip", "gemv_replica.hip", "gemv_lut.hip", "gemm.hip", "gemm_skinny.hip", "gemm_dense.hip", "gemm_tiles.hip", "attn.hip", "attn_channel.hip", "kv_quantize.hip", "attn_paged.hip", "pages.hip", "reorder.hip"]
+SOURCES = ["api.hip", "dequant.hip", "gemv.hip", "gemv_packed.hip", "gemv_mfma.hip", "gemv_replica.hip", "gemv_lut.hip", "gemm.hip", "gemm_skinny.hip", "gemm_dense.hip", "gemm_tiles.hip", "attn.hip", "attn_channel.hip", "kv_quantize.hip", "attn_paged.hip", "attn_paged_few.hip", "pages.hip", "reorder.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are disabled for every kernel of this library

@@ -22,408 +22,13 @@
 // (a round: one tile per wavefront), so that few rows fill the workgroup and many are not joined at the end.  Blocks of a request go in pairs (the last with the
 // first, ...), whose rounds add up to nearly the same number C: the work before a block is a product, not a sum, and every workgroup finds its share
 // with one scan over the requests.  A block cut by a share's border leaves its sums in ws, and attn_paged_merge_kernel joins them in order.
-#include <cfloat>
-#include <climits>
-#include <type_traits>
-
-#include "vq_common.h"
+#include "attn_paged.h"
 
 namespace vq {
 
+using namespace paged;
+
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 8, kThreads = kWaves * 64;
-constexpr int kSide = 65536;                  // LDS of a side's codebooks
-constexpr int kJoinOff = 2 * kSide;           // sums of wavefronts that share rows, 2 KiB each
-constexpr int kStatOff = kJoinOff + 16384;    // their maxima and sums of weights, [wave][32] each
-constexpr int kScanOff = kStatOff + 2048;
-constexpr int kListOff = kScanOff + 256;      // pieces of the share, 64 at a time: their first rounds, and a Piece each
-constexpr int kBaseOff = kListOff + 256 + 64 * 64;   // where the codes of the next rounds lie, [wave][64]
-constexpr int kLds = kBaseOff + kWaves * 64 * 8;
-constexpr float kHeadroom = 6.f, kRise = 8.f; // (log2)
-
-struct PagedArgs {
-    const uint8_t *k_codes, *v_codes;
-    const half_t *k_cb, *v_cb;
-    const int *table, *cu_new, *seq_lens, *prefix_lens;
-    const float *slopes;
-    const half_t *q;
-    half_t *out;
-    float *ws;
-    size_t q_stride, out_stride;
-    int B, H, group, E, G, pg_shift, n_pages, max_pages, log_ps, n_tokens, window;
-    unsigned group_inverse;   // row / group = row * group_inverse >> group_shift, for rows below 2^31
-    int group_shift;
-    int workers;        // workgroups of a cache head
-    int min_log_ways;   // fewest wavefronts that share 32 rows
-    int cut;            // 0: blocks are not cut
-    int min_share;      // rounds
-    float scale2;       // |sm_scale| log2(e)
-    unsigned q_sign;    // sign of sm_scale, in both halves
-    float cap_in, cap_out;   // softcap: cap_out - 2 cap_out / (2^(s cap_in) + 1), 0: none
-};
-
-__device__ __forceinline__ int token_of(const PagedArgs &a, int row) { return (int)(((unsigned long long)(unsigned)row * a.group_inverse) >> a.group_shift); }
-
-// A request, in numbers that fit no memory access out of bounds.
-struct Request {
-    int first, n, len, prefix, rows, log_ways, blocks, items, C;
-};
-// Tiles of 32 keys that some of the tokens [i0, i1] attends: [0, front) and [lo, hi).
-struct Tiles {
-    int front, lo, hi;
-    __device__ int count() const { return front + max(hi - lo, 0); }
-};
-__device__ __forceinline__ Tiles tiles_of(const PagedArgs &a, const Request &r, int i0, int i1) {
-    const int p0 = r.len - r.n + i0, p1 = r.len - r.n + i1;
-    Tiles t;
-    t.lo = (a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0) >> 5;
-    t.hi = (max(p1 + 1, r.prefix) + 31) >> 5;
-    t.front = min((r.prefix + 31) >> 5, t.lo);
-    return t;
-}
-__device__ __forceinline__ int block_rows(const Request &r) { return (kWaves * 32) >> r.log_ways; }
-__device__ __forceinline__ Tiles block_tiles(const PagedArgs &a, const Request &r, int j) {
-    const int row = j * block_rows(r);
-    return tiles_of(a, r, token_of(a, row), token_of(a, min(row + block_rows(r), r.rows) - 1));
-}
-__device__ __forceinline__ int block_rounds(const PagedArgs &a, const Request &r, int j) {   // (a block that attends nothing writes zeros)
-    return max((block_tiles(a, r, j).count() + (1 << r.log_ways) - 1) >> r.log_ways, 1);
-}
-__device__ __forceinline__ Request request_of(const PagedArgs &a, int b) {
-    Request r;
-    const int c0 = min(max(a.cu_new[b], 0), a.n_tokens), c1 = min(max(a.cu_new[b + 1], 0), a.n_tokens);
-    r.first = c0;
-    r.n = max(c1 - c0, 0);
-    r.len = min(max(a.seq_lens[b], 0), a.max_pages << a.log_ps);
-    r.prefix = a.prefix_lens ? min(max(a.prefix_lens[b], 0), r.len) : 0;
-    r.rows = r.n * a.group;
-    r.log_ways = max(r.rows <= 32 ? 3 : r.rows <= 64 ? 2 : r.rows <= 128 ? 1 : 0, a.min_log_ways);
-    r.blocks = (r.rows + block_rows(r) - 1) / block_rows(r);
-    r.items = (r.blocks + 1) / 2;
-    r.C = r.blocks == 0 ? 0 : block_rounds(a, r, 0);
-    if (r.blocks > 1) r.C = max(r.C + block_rounds(a, r, r.blocks - 1), 2 * block_rounds(a, r, r.blocks / 2)) + 1;
-    return r;
-}
-
-__device__ __forceinline__ long long shfl_ll(long long v, int from) {
-    return ((long long)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, from);
-}
-
-// The share of worker w: rounds [u0, u1) of the head's, the first of them round x of request b.  False: none.  All threads of the
-// workgroup call it; xs: LDS, threads / 64 + 2 values.
-struct Share {
-    long long u0, u1, share, x;
-    int b;
-};
-template <int THREADS>
-__device__ __forceinline__ bool find_share(const PagedArgs &a, int w, long long *xs, Share *out) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    constexpr int NW = THREADS / 64;
-    auto share_of = [&](long long total) {
-        out->share = max((total + a.workers - 1) / a.workers, (long long)a.min_share);
-        out->u0 = w * out->share;
-        out->u1 = min(out->u0 + out->share, total);
-        return out->u0 < total;
-    };
-    if (a.B <= 64) {   // every wavefront for itself
-        long long own = 0;
-        if (lane < a.B) {
-            const Request r = request_of(a, lane);
-            own = (long long)r.items * r.C;
-        }
-        long long upto = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const long long y = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += y;
-        }
-        if (!share_of(shfl_ll(upto, 63))) return false;
-        out->b = __ffsll((long long)__ballot(out->u0 < upto)) - 1;
-        out->x = out->u0 - shfl_ll(upto - own, out->b);
-        return true;
-    }
-    long long mine = 0, total = 0, own = 0;
-    for (int b = tid; b < a.B; b += THREADS) {
-        const Request r = request_of(a, b);
-        own = (long long)r.items * r.C;
-        mine += own;
-    }
-    long long incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const long long y = __shfl_up(incl, d, 64);
-        if (lane >= d) incl += y;
-    }
-    if (lane == 63) xs[wave] = incl;
-    __syncthreads();
-    long long before = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        if (i < wave) before += xs[i];
-        total += xs[i];
-    }
-    incl += before;
-    if (!share_of(total)) return false;
-    __syncthreads();
-    if (a.B <= THREADS) {
-        if (incl - mine <= out->u0 && out->u0 < incl) {
-            xs[NW] = tid;
-            xs[NW + 1] = out->u0 - (incl - mine);
-        }
-    } else {
-        long long carry = 0;
-        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-            const int b = b0 + tid;
-            long long u = 0;
-            if (b < a.B) {
-                const Request r = request_of(a, b);
-                u = (long long)r.items * r.C;
-            }
-            long long in = u, chunk = 0, lower = 0;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const long long y = __shfl_up(in, d, 64);
-                if (lane >= d) in += y;
-            }
-            if (lane == 63) xs[wave] = in;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                if (i < wave) lower += xs[i];
-                chunk += xs[i];
-            }
-            __syncthreads();
-            const long long from = carry + lower + in - u;
-            if (from <= out->u0 && out->u0 < from + u) {
-                xs[NW] = b;
-                xs[NW + 1] = out->u0 - from;
-            }
-            carry += chunk;
-        }
-    }
-    __syncthreads();
-    const long long b = xs[NW], x = xs[NW + 1];
-    out->b = __builtin_amdgcn_readfirstlane((int)b);
-    out->x = ((long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
-    return true;
-}
-
-// Rounds [r0, r1) of a block of a request.
-struct alignas(16) Piece {
-    int first, pos0, len, prefix;       // of the request: its first row of q, length before its new tokens, length, prefix
-    int rows, log_ways, row0, b;        // rows of the request, first row of the block
-    int front, lo, count, whole;        // tiles of the block: [0, front) and [lo, ...), count in all; r0 .. r1 is all of it
-    int r0, r1, pad0, pad1;
-};
-__device__ __forceinline__ Piece uniform_piece(const Piece &p) {
-    Piece u;
-    constexpr int N = sizeof(Piece) / 4;
-    int t[N];
-    __builtin_memcpy(t, &p, sizeof(Piece));
-#pragma unroll
-    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_readfirstlane(t[i]);
-    __builtin_memcpy(&u, t, sizeof(Piece));
-    return u;
-}
-
-// The next pieces of a share, 64 at most: from round *x of request *b on, *left rounds; all three step behind them.  A lane makes a piece:
-// of one request (as many as have a single block), or of one block of a larger request.  Every wavefront of the workgroup makes the same list,
-// one writes it.  Returns the pieces; *rounds: theirs, each piece's rounded up to PAD.
-template <int PAD>
-__device__ __forceinline__ int list_pieces(const PagedArgs &a, int *b, long long *x, long long *left, bool write, int *starts, Piece *list, int *rounds) {
-    const int lane = threadIdx.x & 63;
-    Request r = {};
-    if (*b + lane < a.B) r = request_of(a, *b + lane);
-    Piece pc = {};
-    int from, to, j = 0, off = 0, n = 0;   // rounds [from, to) of the item; the block's first in it, the block's number of them
-    bool there;
-    const unsigned long long large = __ballot(r.blocks > 1);
-    if (large & 1) {
-        Request u;
-        constexpr int N = sizeof(Request) / 4;
-        int t[N];
-        __builtin_memcpy(t, &r, sizeof(Request));
-#pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_readfirstlane(t[i]);
-        __builtin_memcpy(&u, t, sizeof(Request));
-        r = u;
-        const int k0 = (int)(*x / r.C), from0 = (int)(*x - (long long)k0 * r.C), ahead = lane >> 1, k = k0 + ahead;
-        const long long before = ahead == 0 ? 0 : (long long)ahead * r.C - from0;
-        from = ahead == 0 ? from0 : 0;
-        to = from + (int)min(max(*left - before, 0ll), (long long)(r.C - from));
-        there = k < r.items && to > from;
-        if (there) {
-            const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
-            j = (lane & 1) ? k : jl;
-            off = (lane & 1) ? nl : 0;
-            n = (lane & 1) ? block_rounds(a, r, k) : nl;
-            there = !((lane & 1) && k == jl);
-        }
-        const long long taken = min(*left, (long long)(min(k0 + 32, r.items) - k0) * r.C - from0);
-        *left -= taken;
-        *x += taken;
-        pc.b = *b;
-        if (*x == (long long)r.items * r.C) {
-            *x = 0;
-            *b += 1;
-        }
-    } else {
-        const int simple = large ? __ffsll((long long)large) - 1 : 64;
-        from = lane == 0 ? (int)*x : 0;
-        const int avail = lane < simple ? r.items * r.C - from : 0;
-        long long upto = avail;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const long long y = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += y;
-        }
-        to = from + (int)min(max(*left - (upto - avail), 0ll), (long long)avail);
-        there = to > from;
-        n = there ? block_rounds(a, r, 0) : 0;
-        *left -= min(*left, shfl_ll(upto, 63));
-        pc.b = *b + lane;
-        *x = 0;
-        *b += simple;
-    }
-    if (a.cut) {
-        pc.r0 = max(from - off, 0);
-        pc.r1 = to == r.C ? n : min(to - off, n);
-    } else {   // whole blocks, with the share that they begin in
-        pc.r0 = 0;
-        pc.r1 = off >= from && (off < to || to == r.C) ? n : 0;
-    }
-    there = there && pc.r0 < pc.r1;
-    pc.whole = pc.r0 == 0 && pc.r1 == n;
-    const int mine = there ? (pc.r1 - pc.r0 + PAD - 1) / PAD * PAD : 0;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(upto, d, 64);
-        if (lane >= d) upto += y;
-    }
-    *rounds = __builtin_amdgcn_readlane(upto, 63);
-    const unsigned long long all = __ballot(there);
-    if (write && there) {
-        const Tiles t = block_tiles(a, r, j);
-        pc.first = r.first;
-        pc.pos0 = r.len - r.n;
-        pc.len = r.len;
-        pc.prefix = r.prefix;
-        pc.rows = r.rows;
-        pc.log_ways = r.log_ways;
-        pc.row0 = j * block_rows(r);
-        pc.front = t.front;
-        pc.lo = t.lo;
-        pc.count = t.count();
-        pc.pad0 = pc.pad1 = 0;
-        const int at = __popcll(all & ((1ull << lane) - 1ull));
-        starts[at] = upto - mine;
-        list[at] = pc;
-    }
-    return __popcll(all);
-}
-
-// Sums of cut blocks: two per worker (the block that its share begins inside, the one that it ends inside), [rows][D] and [rows][2].
-__device__ __forceinline__ size_t part_of(const PagedArgs &a, int h, int w, int which) { return ((size_t)h * a.workers + w) * 2 + which; }
-__host__ __device__ __forceinline__ int part_rows(const PagedArgs &a) { return (kWaves * 32) >> a.min_log_ways; }
-template <int D>
-__device__ __forceinline__ float *part_sums(const PagedArgs &a, size_t part) { return a.ws + part * part_rows(a) * D; }
-template <int D>
-__device__ __forceinline__ float *part_stats(const PagedArgs &a, size_t part) {
-    return a.ws + (size_t)a.H * a.workers * 2 * part_rows(a) * D + part * part_rows(a) * 2;
-}
-
-template <int BYTES>
-struct Raw;
-template <>
-struct Raw<16> { typedef unsigned type __attribute__((ext_vector_type(4))); };
-template <>
-struct Raw<8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
-template <>
-struct Raw<4> { typedef unsigned type; };
-
-// BYTES from an LDS byte address to dwords
-template <int BYTES>
-__device__ __forceinline__ void lds_read(unsigned addr, uint32_t *to) {
-    typedef typename Raw<BYTES>::type raw_t;
-    const raw_t r = *reinterpret_cast<const __attribute__((address_space(3))) raw_t *>((uintptr_t)addr);
-    __builtin_memcpy(to, &r, BYTES);
-}
-// ds_read_b64_tr_b16: of each group of 16 lanes, lane l gets half l % 4 of what lanes l / 4, 4 + l / 4, 8 + l / 4 and 12 + l / 4 ask for
-__device__ __forceinline__ void lds_read_transposed(unsigned addr, uint32_t *to) {
-    typedef short raw_t __attribute__((ext_vector_type(4)));
-    const raw_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<raw_t __attribute__((address_space(3))) *>((uintptr_t)addr));
-    __builtin_memcpy(to, &r, 8);
-}
-template <int BYTES>
-__device__ __forceinline__ typename Raw<BYTES>::type global_read(const void *p) {
-    return *reinterpret_cast<const typename Raw<BYTES>::type *>(p);
-}
-
-// byte B of w in bits 8 .. 15, the lane's constant around it
-template <int B>
-__device__ __forceinline__ unsigned row_address(uint32_t w, unsigned lane_const) {
-    return __builtin_amdgcn_perm(w, lane_const, 0x0c020000u | ((4u + B) << 8));
-}
-
-// One side's codebooks of a head (cb) for LDS: load() requests them, store() writes them.  By entry: every entry 256 / (2 v) times in a row of
-// 256 bytes, or a table per sub-vector.  By position (v = 2, values): row e holds entry e for all 32 positions of the operand.  Rows of
-// entries that do not exist are zero.
-template <int D, int V, bool COPIES, bool POSITIONS>
-struct Tables {
-    static constexpr int ES = 2 * V, P = D / V, CH = D / 32;
-    static constexpr int US = POSITIONS ? 2 * (V < CH ? V : CH) : ES;      // bytes of a unit of memory
-    static constexpr int UNITS = 2 * D / US;                               // POSITIONS: units of a row
-    static constexpr int N = (POSITIONS ? 256 * UNITS : COPIES ? 256 * 16 : P * 256) / kThreads;
-    typedef typename Raw<US>::type unit_t;
-    unit_t u[N];
-
-    static __device__ __forceinline__ void place(int at, int *row, int *unit) {
-        if (!POSITIONS) {
-            *row = COPIES ? at >> 4 : at & 255;
-            *unit = COPIES ? 0 : at >> 8;
-        } else if (COPIES) {   // neighbours read one entry
-            *row = at / UNITS;
-            *unit = at % UNITS;
-        } else {               // eight entries of eight positions: 64-byte pieces from memory, eight columns of LDS
-            *row = (at >> 3) / UNITS * 8 + (at & 7);
-            *unit = (at >> 3) % UNITS;
-        }
-    }
-    __device__ __forceinline__ void load(const PagedArgs &a, const unsigned char *cb, int tid) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            int row, unit;
-            place(tid + i * kThreads, &row, &unit);
-            const int ch = POSITIONS ? unit * (US / 2) : unit * V, p = COPIES ? 0 : (ch / V) >> a.pg_shift;
-            u[i] = global_read<US>(cb + (unsigned)((p * a.E + min(row, a.E - 1)) * ES + (POSITIONS ? ch % V * 2 : 0)));
-        }
-    }
-    __device__ __forceinline__ void store(const PagedArgs &a, unsigned char *to, int tid) const {
-        const unit_t none = {};
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = tid + i * kThreads;
-            int row, unit;
-            place(at, &row, &unit);
-            const unit_t x = row < a.E ? u[i] : none;
-            if (POSITIONS) {
-                *reinterpret_cast<unit_t *>(to + row * 256 + unit * US) = x;
-            } else if (COPIES) {
-                unit_t r[16 / US];
-#pragma unroll
-                for (int k = 0; k < 16 / US; ++k) r[k] = x;
-                uint4 q;
-                __builtin_memcpy(&q, r, 16);
-                reinterpret_cast<uint4 *>(to)[at] = q;
-            } else {
-                reinterpret_cast<unit_t *>(to)[at] = x;
-            }
-        }
-    }
-};
 
 template <int D, int V, bool COPIES, bool MODS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_paged_kernel(PagedArgs a) {
@@ -569,7 +174,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             const int pos_f = pc.pos0 + token_of(a, max(row0, 0)), pos_l = pc.pos0 + token_of(a, max(row0 + tile_rows - 1, 0));
             const int count = tile_rows > 0 ? min(pc.front + max(((max(pos_l + 1, pc.prefix) + 31) >> 5) - pc.lo, 0), pc.count) : 0;
             const float slope2 = MODS && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
-            const int see_to = min(pos, pc.len - 1), see_from = a.window > 0 ? pos - a.window + 1 : INT_MIN;
+            const int see_to = min(pos, pc.len - 1), see_from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
 
             // This wavefront's tiles: idx0, idx0 + ways, ...
             const int idx0 = (pc.r0 << pc.log_ways) + kw, rounds = pc.r1 - pc.r0;
@@ -624,12 +229,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     }
                 }
                 if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
+                    const int see = attended_keys(t0 + 16 * lh, see_from, see_to, pc.prefix);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int key = t0 + 16 * lh + 4 * (e & 3) + (e >> 2);
-                        const bool see = (key <= see_to && key >= see_from) || key < pc.prefix;
-                        s[e] = see ? s[e] : -INFINITY;
-                    }
+                    for (int e = 0; e < 16; ++e) s[e] = attended(s[e], see, 4 * (e & 3) + (e >> 2));
                 }
                 // running maximum (a NaN raises nothing: its row's weights are NaN by themselves)
                 float mt = s[0];
@@ -850,104 +452,40 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
-constexpr int kMergeRows = 32;   // of a workgroup
-// Joins the sums of the block that worker w's share begins inside, if no worker before it began there too.
-template <int D>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedArgs a) {
-    __shared__ long long xs[256 / 64 + 2];
-    const int w = blockIdx.x + 1, h = blockIdx.y, tid = threadIdx.x;
-    Share sh;
-    if (!find_share<256>(a, w, xs, &sh)) return;
-    const Request r = request_of(a, sh.b);
-    const int k = (int)(sh.x / r.C), from = (int)(sh.x - (long long)k * r.C);
-    const int jl = r.blocks - 1 - k, nl = block_rounds(a, r, jl);
-    int j = jl, off = 0, rounds = nl;
-    if (from >= nl) {
-        if (k == jl) return;
-        j = k;
-        off = nl;
-        rounds = block_rounds(a, r, k);
-    }
-    if ((int)blockIdx.z * kMergeRows >= block_rows(r) || from <= off || from >= off + rounds || from - sh.share > off) return;
-    // pieces: the end of worker w - 1's share, then the beginnings of w's and of those behind it that begin inside the block
-    const long long end = sh.u0 - from + min(off + rounds, r.C);
-    const int pieces = 1 + (int)((end - sh.u0 + sh.share - 1) / sh.share);
-    const int row0 = j * block_rows(r), rows = min(block_rows(r), r.rows - row0);
-    constexpr int PER = D / 8;   // threads of a row
-    for (int t = tid; t < kMergeRows * PER; t += 256) {
-        const int lr = blockIdx.z * kMergeRows + t / PER, ch = t % PER * 8, row = row0 + lr;
-        if (lr >= rows) break;
-        // (four pieces at a time are requested at once: each is a trip to memory, or two)
-        constexpr int N = 4;
-        auto part = [&](int p) { return part_of(a, h, w - 1 + p, p == 0 ? 1 : 0); };
-        float M = -FLT_MAX, L = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int p0 = 0; p0 < pieces; p0 += N) {
-            float m[N], l[N];
-            float4_t y[N][2];
-#pragma unroll
-            for (int p = 0; p < N; ++p) {   // (past the end: the last one once more, without weight)
-                const size_t from = part(min(p0 + p, pieces - 1));
-                const float *st = part_stats<D>(a, from) + lr * 2;
-                m[p] = st[0];
-                l[p] = st[1];
-                const float4_t *sums = reinterpret_cast<const float4_t *>(part_sums<D>(a, from) + (size_t)lr * D + ch);
-                y[p][0] = sums[0];
-                y[p][1] = sums[1];
-            }
-            float top = M;
-#pragma unroll
-            for (int p = 0; p < N; ++p) top = fmaxf(top, m[p]);
-            const float keep = __builtin_amdgcn_exp2f(M - top);
-            M = top;
-            L *= keep;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= keep;
-#pragma unroll
-            for (int p = 0; p < N; ++p) {
-                if (p0 + p >= pieces) break;
-                const float f = __builtin_amdgcn_exp2f(m[p] - M);
-                L += l[p] * f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] += y[p][e / 4][e % 4] * f;
-            }
-        }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        half8_t y;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (half_t)(x[e] * inv);
-        const int i = token_of(a, row), hq = h * a.group + (row - i * a.group);
-        *reinterpret_cast<half8_t *>(a.out + (size_t)(r.first + i) * a.out_stride + (size_t)hq * D + ch) = y;
-    }
-}
-
 // How a call is cut, from its sizes alone.
 struct PagedPlan {
-    int workers, min_log_ways, cut;
+    int few, workers, min_log_ways, cut;
     size_t ws;
 };
 PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     PagedPlan p;
     p.workers = kv->H >= 256 ? 1 : 256 / kv->H;
     const long long rows = (long long)b->n_tokens * (b->Hq / kv->H) * kv->H;
-    p.min_log_ways = rows >= 256 * 1024 ? 0 : rows >= 128 * 1024 ? 1 : 2;
+    // Tiles of 16 rows and 64 keys for requests of 16 rows on average at most, where there is enough to read: a tile takes about as long as
+    // one of 32 rows and 32 keys, so long caches take less (us of both, few rows first; H = 32, a row a request: 16 requests of 16384 tokens
+    // 132 and 150, 64 of 4096 154 and 165; H = 8, 16 rows a request: 64 of 16384 125 and 163, 64 of 1024 32 and 44), but a
+    // wavefront alone with a larger tile is later with it (one of 300 tokens 17 and 13, H = 32; 16 of 2048 42 and 38).  The wider
+    // tiles take longer per row beyond four (their sums join in more steps), so there it pays earlier.
+    const long long keys = (long long)b->B * kv->H * b->max_pages * kv->page_tokens, few_rows = (long long)b->n_tokens * (b->Hq / kv->H);
+    p.few = few_supported(kv->D, kv->v) && few_rows <= 16ll * b->B && keys >= (few_rows > 4ll * b->B ? 1ll << 18 : 1ll << 21);
+    p.min_log_ways = p.few ? 3 : rows >= 256 * 1024 ? 0 : rows >= 128 * 1024 ? 1 : 2;
     p.cut = p.workers > 1 && (long long)b->max_pages * kv->page_tokens > 512;
-    p.ws = p.cut ? (size_t)kv->H * p.workers * 2 * ((kWaves * 32) >> p.min_log_ways) * (kv->D + 2) * sizeof(float) : 0;
+    p.ws = p.cut ? (size_t)kv->H * p.workers * 2 * ((kWaves * (p.few ? 16 : 32)) >> p.min_log_ways) * (kv->D + 2) * sizeof(float) : 0;
     return p;
 }
 
 template <int D, int V, bool COPIES, bool MODS>
-int run_paged(const PagedArgs &a, hipStream_t s) {
+int run_wide(const PagedArgs &a, hipStream_t s) {
     static KernelSetup setup;
     if (int st = kernel_setup(reinterpret_cast<const void *>(&attn_paged_kernel<D, V, COPIES, MODS>), kLds, true, setup)) return st;
     attn_paged_kernel<D, V, COPIES, MODS><<<a.H * a.workers, kThreads, kLds, s>>>(a);
-    if (a.cut) attn_paged_merge_kernel<D><<<dim3(a.workers - 1, a.H, part_rows(a) / kMergeRows), 256, 0, s>>>(a);
-    return launch_status();
+    return merge<D>(a, s);
 }
 template <int D, int V>
 int run_paged_as(const PagedArgs &a, hipStream_t s) {
     const bool mods = a.cap_out > 0.f || a.slopes;
-    if (a.G == 1) return mods ? run_paged<D, V, true, true>(a, s) : run_paged<D, V, true, false>(a, s);
-    return mods ? run_paged<D, V, false, true>(a, s) : run_paged<D, V, false, false>(a, s);
+    if (a.G == 1) return mods ? run_wide<D, V, true, true>(a, s) : run_wide<D, V, true, false>(a, s);
+    return mods ? run_wide<D, V, false, true>(a, s) : run_wide<D, V, false, false>(a, s);
 }
 
 }  // namespace
@@ -992,6 +530,8 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.n_tokens = b->n_tokens;
     a.window = b->window < b->max_pages * kv->page_tokens ? b->window : 0;   // (one that reaches every token is none)
     a.workers = p.workers;
+    a.tile_rows = p.few ? 16 : 32;
+    a.log_keys = p.few ? 6 : 5;
     a.min_log_ways = p.min_log_ways;
     a.cut = p.cut;
     a.min_share = 2;
@@ -1000,6 +540,7 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;
     a.cap_out = b->softcap * kLog2e;
     a.cap_in = b->softcap > 0.f ? 2.f * a.scale2 / b->softcap : 0.f;
+    if (p.few) return launch_few(a, kv->v, s);
     if (kv->D == 64) return kv->v == 8 ? run_paged_as<64, 8>(a, s) : kv->v == 4 ? run_paged_as<64, 4>(a, s) : run_paged_as<64, 2>(a, s);
     return kv->v == 8 ? run_paged_as<128, 8>(a, s) : kv->v == 4 ? run_paged_as<128, 4>(a, s) : run_paged_as<128, 2>(a, s);
 }

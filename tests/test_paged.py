@@ -487,6 +487,72 @@ def test_attend_head_counts(gpu_device, H, group):
     check(case, attend(case, gpu_device))
 
 
+# Requests of few rows on tables that may name many pages take narrower tiles: B H max_pages page_tokens of 2^21 and more.
+def on_a_wide_table(case):
+    W = -(-(1 << 21) // (len(case.reqs) * case.H * case.ps))
+    assert case.rows * case.group <= 16 * len(case.reqs) and W >= case.table.shape[1]
+    wide = np.full((len(case.reqs), W), -1, np.int32)
+    wide[:, :case.table.shape[1]] = case.table
+    case.table = wide
+    workers = max(256 // case.H, 1)
+    kv, q, table = case.dev("cuda")[:3]
+    assert vq.vq_attn_paged_workspace(kv, q, table) == case.H * workers * 2 * 16 * (case.D + 2) * 4
+    return case
+
+
+@gpu
+@pytest.mark.parametrize("lens", [[1], [2, 15, 16, 17], [31, 32, 33, 63, 64, 65], [127, 128, 129, 511, 512, 513], [1000, 1, 1537]])
+@pytest.mark.parametrize("v,G,group,ps", [(4, 1, 1, 16), (4, 32, 3, 16), (8, 1, 16, 64), (8, 16, 5, 32), (4, 8, 9, 128), (8, 2, 2, 16)])
+def test_attend_few_rows_single_tokens(gpu_device, lens, v, G, group, ps):
+    case = on_a_wide_table(Case([(ln, 1) for ln in lens], v=v, G=G, group=group, ps=ps, seed=len(lens) + v))
+    check(case, attend(case, gpu_device))
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(window=1), dict(window=63), dict(window=64), dict(window=200), dict(window=20, prefix=[5, 0, 300, 40, 0, 1]),
+                                dict(prefix=[70, 1, 33, 1000, 0, 7]), dict(softcap=5.0), dict(softcap=30.0, window=40), dict(slopes=True),
+                                dict(slopes=True, prefix=[90, 9, 2, 64, 0, 65], window=17, softcap=2.0), dict(sm_scale=-0.3), dict(sm_scale=0.0), dict(sm_scale=1.5)])
+@pytest.mark.parametrize("v,G", [(4, 1), (4, 32), (8, 1), (8, 8)])
+def test_attend_few_rows_masks_and_scores(gpu_device, kw, v, G):
+    """One of the requests has more rows than a tile, one no new tokens, one rows before its first token."""
+    kw = dict(kw)
+    if kw.get("slopes"):
+        kw["slopes"] = [0.5, 0.01, 2.0, -0.02]
+    case = on_a_wide_table(Case([(120, 23), (17, 0), (700, 1), (64, 3), (3, 8), (0, 0)], H=2, group=2, v=v, G=G, seed=3, extra_rows=2, **kw))
+    check(case, attend(case, gpu_device))
+
+
+@gpu
+@pytest.mark.parametrize("reqs,kw", [
+    ([(9000, 1)], dict(H=1, group=1)), ([(5000, 3), (12000, 1), (40, 1)], dict(H=2, group=2, G=32)), ([(3000, 1), (1, 1)], dict(H=3, group=15, v=8, ps=64)),
+    ([(4000, 1)] * 5 + [(100, 1)] * 3, dict(H=1, group=8, v=8)), ([(6000, 5)], dict(H=1, group=1, window=2500, prefix=[100], v=8, G=16)),
+    ([(300, 1)] * 70, dict(H=1, group=2)), ([(4000, 40)] + [(50, 1)] * 20, dict(H=1, group=1, v=8)), ([(900, 1)], dict(H=300, group=5, v=8))])
+def test_attend_few_rows_long_and_many_requests(gpu_device, reqs, kw):
+    case = Case(reqs, seed=11, **kw)
+    check(case, attend(on_a_wide_table(case) if case.H < 256 else case, gpu_device))     # (a head per workgroup: five rows are enough)
+
+
+@gpu
+@pytest.mark.parametrize("v,G", [(4, 1), (8, 16)])
+def test_attend_few_rows_growing_scores_and_values_that_are_none(gpu_device, v, G):
+    """The largest score comes last; codes behind the end name entries that are infinite or NaN; a NaN in a query stays in its row."""
+    case = Case([(1501, 2), (90, 1)], H=1, group=2, v=v, G=G, E=200, seed=6, sm_scale=2.0)
+    order = np.argsort(case.values(case.K_codes[0], case.k_cb)[:, 0] @ case.q[0, 0].astype(np.float64))
+    case.K_codes[0] = case.K_codes[0][order]
+    t = np.arange(1501)
+    case.k_codes[case.table[0, t // 16], :, t % 16] = case.K_codes[0]
+    want = attend(on_a_wide_table(case), gpu_device)
+    check(case, want)
+    wider = [np.concatenate([cb, np.full((1, G, 56, v), x, np.float16)], 2) for cb, x in ((case.k_cb, np.nan), (case.v_cb, np.inf))]
+    case.k_cb, case.v_cb = wider
+    assert torch.equal(attend(case, gpu_device), want)     # (256 entries: any byte behind the end is one)
+    case.q[1, 1, 3] = np.nan
+    got = attend(case, gpu_device)
+    assert bool(torch.isnan(got[1, 1]).all())
+    got[1, 1] = want[1, 1]
+    assert torch.equal(got, want)
+
+
 @gpu
 def test_attend_many_requests(gpu_device):
     rng = np.random.Generator(np.random.PCG64(4))
