@@ -468,6 +468,9 @@ int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_st
  * make the call read or write out of bounds, but leave the request's rows unspecified.
  * The requests' key ranges are cut into equal shares for the compute units; a share's sums are joined by log-sum-exp in a second
  * launch, in a fixed order: repeated calls are bit-identical.  ws: vq_attn_paged_workspace(kv, batch) bytes; the query reads only sizes.
+ * Calls that may overlap (other streams, graphs that are replayed side by side) must not share ws.  Sizes alone choose the kernel and the shares
+ * (not the lengths, which the host does not know): B * max_pages * page_tokens counts as what there is to read, so a table far wider
+ * than the requests are long may cost a few microseconds, and last bits may differ between tables of other widths.
  * n_pages >= 1; D is 64 or 128, D / v / cb_groups a power of two (VQ_ERR_UNSUPPORTED otherwise).
  */
 typedef struct vq_paged_batch_t {

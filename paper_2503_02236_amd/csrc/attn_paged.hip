@@ -4,24 +4,34 @@
 // tiles of 32 cached tokens with the running maximum m, sum l and accumulators of a softmax:
 //   S^T = K Q^T   v_mfma_f32_32x32x16_f16, operand A = K: lane (key, half) takes 8 channels of its key, gathered by code from the
 //                 codebook in LDS straight into the operand.  Which key a row of the operand is, and which channel a step, is free: row
-//                 16 s + 8 a + 4 l + j is key 16 s + 8 l + 4 a + j, and half l takes the channels of its half of the head, so that a lane's codes are
-//                 consecutive bytes and its scores are those of the keys 16 s + 8 l + (0 .. 7) of one row;
-//   O^T = V^T P^T with P^T as operand B: exactly those scores, after exp2, as halves: no shuffle, no LDS.  Operand A = V^T: the lane
-//                 takes the channels of one position for its 8 keys (8 consecutive bytes of codes: the layout of the value pages), and
-//                 permutes the gathered pairs into D / 32 operands.
-// A weight is 2^(s - m + 6) rounded to a half (relative error 2^-11; the sum l takes it unrounded): m follows the maximum only when
-// that has grown by more than 8, so weights lie below 2^14 and those that fall below a half's range are below 2^-31 of the largest.
-// Sums, statistics and outputs before the last rounding are fp32.
+//                 8 a + 4 b + c is key 16 b + 4 c + a, and half l takes the channels of its half of the head, so that a lane's codes are
+//                 consecutive bytes, and its 16 scores are those of the 16 consecutive keys of block l, score e that of key 4 (e % 4) + e / 4;
+//   O^T = V^T P^T with P^T as operand B: exactly those scores, after exp2, as halves: no shuffle, no LDS.  Operand A = V^T: for v = 4 and 8 a
+//                 lane asks for the entries of four consecutive tokens (a dword of codes: the layout of the value pages) at its positions, and
+//                 the transposing LDS read hands them out by channel; for v = 2 a lane reads its channels' pairs for the block's
+//                 tokens and permutes them into operands.
+// A weight is 2^(s - m + 6) rounded to a half (relative error 2^-11, what the matrix instruction takes; the sum l adds the rounded ones, so
+// that weights add up to one): m follows the maximum only when that has grown by more than 8, so weights lie below 2^14 and those
+// that fall below a half's range are below 2^-31 of the largest.  Sums, statistics and outputs before the last rounding are fp32.
 //
-// Codebooks in LDS (64 KiB a side).  V: row e holds entry e for all 32 channel positions of the operand, so the 32 lanes of a pass
-// read 32 different columns: no bank conflicts, whatever the codebook groups.  K: one codebook per head: every entry
-// 256 / (2 v) times in a row of 256 bytes, lane l reads copy l, again without conflicts; more: a table per sub-vector.
+// Codebooks in LDS (64 KiB a side).  One codebook per head: every entry 256 / (2 v) times in a row of 256 bytes, lane l reads copy l, and no
+// two lanes of a pass meet in a bank (1.6 ns a gather of 8 bytes on a compute unit, 2.2 from a single copy).  More: a table per
+// sub-vector.  Values for v = 2: row e holds entry e for all 32 positions of the operand.
 //
 // Work.  A workgroup of 8 wavefronts (one per compute unit, for its LDS) belongs to a cache head and takes an equal share of the head's
 // work.  A request's rows are cut into blocks of 256 / ways rows; in a block `ways` wavefronts share 32 rows and take every ways-th tile of keys
 // (a round: one tile per wavefront), so that few rows fill the workgroup and many are not joined at the end.  Blocks of a request go in pairs (the last with the
 // first, ...), whose rounds add up to nearly the same number C: the work before a block is a product, not a sum, and every workgroup finds its share
 // with one scan over the requests.  A block cut by a share's border leaves its sums in ws, and attn_paged_merge_kernel joins them in order.
+// The rounds of a share are one sequence over all its blocks: codes are requested NB tiles ahead (pages 32 rounds ahead), across blocks too.
+//
+// What bounds it.  Not memory: codes that lie in L2 take as long as codes from HBM (57 and 61 us where both were timed).  Two wavefronts a SIMD, each
+// with a tile's 16 matrix instructions (18 ns each) and 200 vector instructions (1.9 ns: addresses of the gathers, weights), in order: a chunk of 2048 rows
+// by counters has the matrix units busy for 43 % and the vector units for 49 % of the time, 17 % of it together, at 1.9 GHz; no bank conflicts.
+// A round of 8 tiles takes 1.25 - 1.4 us, and before the first one lie 5 - 6 us: lengths, pages, codebooks, codes, each a trip to memory.
+// 240 GFLOP of a prompt's chunk 0.28 ms (856 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
+// LDS gathers 1458).  One wavefront a SIMD with 64 rows, where every gather is used twice, took 318 - 365 us: a wavefront alone issues at
+// most one instruction in 4.7 clocks.
 #include "attn_paged.h"
 
 namespace vq {
@@ -468,8 +478,14 @@ PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     // tiles take longer per row beyond four (their sums join in more steps), so there it pays earlier.
     const long long keys = (long long)b->B * kv->H * b->max_pages * kv->page_tokens, few_rows = (long long)b->n_tokens * (b->Hq / kv->H);
     p.few = few_supported(kv->D, kv->v) && few_rows <= 16ll * b->B && keys >= (few_rows > 4ll * b->B ? 1ll << 18 : 1ll << 21);
-    p.min_log_ways = p.few ? 3 : rows >= 256 * 1024 ? 0 : rows >= 128 * 1024 ? 1 : 2;
-    p.cut = p.workers > 1 && (long long)b->max_pages * kv->page_tokens > 512;
+    // Wavefronts that share rows read other tiles of keys and join their sums; wavefronts with rows of their own gather the same keys each, and few
+    // rows are few blocks to deal out.  Rows of all heads, us with 1 / 2 / 4 wavefronts a 32 rows: 32768 98 / 99 / 87, 65536 296 / 274 / 283 (2048 new tokens of 8192),
+    // 102400 225 / 238 / 245, 268800 329 / 370 / 474.
+    p.min_log_ways = p.few ? 3 : rows >= 96 * 1024 ? 0 : rows >= 40 * 1024 ? 1 : 2;
+    // Blocks of short requests stay whole: a share's border inside one costs the joining launch, 2 - 5 us, more than the shares' evenness gains.  Whole and
+    // cut, us: 8 requests of 1000 tokens, a new one each, 16.6 and 23.2; 4 of 900 new tokens of 1000, 96 and 108; of 1500 60 and 63; 8 of 2000 19.8 and 24.0, but
+    // 16 of 500 new ones of 2000 268 and 260.
+    p.cut = p.workers > 1 && (long long)b->max_pages * kv->page_tokens > 1536;
     p.ws = p.cut ? (size_t)kv->H * p.workers * 2 * ((kWaves * (p.few ? 16 : 32)) >> p.min_log_ways) * (kv->D + 2) * sizeof(float) : 0;
     return p;
 }
@@ -534,7 +550,7 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.log_keys = p.few ? 6 : 5;
     a.min_log_ways = p.min_log_ways;
     a.cut = p.cut;
-    a.min_share = 2;
+    a.min_share = 2;   // (4 requests of 4096 tokens, 8 heads, us with 1 / 2 / 4 rounds: 21.2 / 20.9 / 25.0; one: 22.8 / 20.8 / 21.2)
     const float scale = sm_scale < 0.f ? -sm_scale : sm_scale;
     a.scale2 = scale * kLog2e > FLT_MIN ? scale * kLog2e : FLT_MIN;   // (above zero: minus infinity times it has to stay)
     a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;

@@ -7,7 +7,9 @@
 //   O^T, step s over the keys whose last two bits are 2 s and 2 s + 1: slot 8 g + 4 j + e of the operands is key 16 g + 4 e + 2 s + j, the lane's own
 //                 score; lane 4 e + c of a group asks for the entries of its four keys 16 g + 4 e + (0 .. 3) -- one dword of codes -- and position block c, part f, and
 //                 the transposing read hands them out by channel.
-// D = 128, v = 4 or 8.
+// D = 128, v = 4 or 8.  A round of 8 tiles takes 1.6 us, of twice the keys that the wider tiles take 1.3 us for.  What is left is what a tile costs whatever its
+// rows: a gather and its address for every 8 bytes of entries (64 of each in 115 vector instructions), and the time until all wavefronts are done with a
+// request (2 - 4 us, its sums 1 us).  16 requests of up to 4096 tokens, 32 heads: 48 us, where their 103 MB of codes would take 15 from HBM.
 #include "attn_paged.h"
 
 namespace vq {

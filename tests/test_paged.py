@@ -533,6 +533,16 @@ def test_attend_few_rows_long_and_many_requests(gpu_device, reqs, kw):
 
 
 @gpu
+@pytest.mark.parametrize("n", [1, 3])
+def test_attend_few_rows_in_whole_blocks(gpu_device, n):
+    """Short requests on a short table: no block is cut, and many workgroups of a head have one or none to begin with."""
+    case = Case([(5 + 3 * b, n) for b in range(100)] + [(9, 0)], H=16, group=5, v=8, seed=n)
+    kv, q, table = case.dev(gpu_device)[:3]
+    assert vq.vq_attn_paged_workspace(kv, q, table) == 0 and table.numel() * case.ps * case.H >= 1 << 18
+    check(case, attend(case, gpu_device))
+
+
+@gpu
 @pytest.mark.parametrize("v,G", [(4, 1), (8, 16)])
 def test_attend_few_rows_growing_scores_and_values_that_are_none(gpu_device, v, G):
     """The largest score comes last; codes behind the end name entries that are infinite or NaN; a NaN in a query stays in its row."""
