@@ -462,7 +462,7 @@ int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_st
  *   visible(t) = t < seq_lens[b] and ( t <= pos and (window == 0 or t > pos - window)  or  t < prefix_lens[b] )
  *   out     = softmax over the visible t of s(t) . V[b][h][t]; zeros where nothing is visible
  * Rows of q and out behind cu_new[B] are neither read nor written.
- *   q, out: device fp16, token i's head hq at element i * stride + hq * D (strides >= Hq * D, multiples of 8).
+ *   q, out: device fp16, token i's head hq at element i * stride + hq * D (strides >= Hq * D, multiples of 8); they must not overlap.
  * Tokens that a row does not attend never matter, with whatever codes behind a request's length; entries that codes of
  * its tokens point at have to be finite.  Page ids outside [0, n_pages), lengths beyond the table and cu_new beyond n_tokens do not
  * make the call read or write out of bounds, but leave the request's rows unspecified.

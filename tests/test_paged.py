@@ -426,6 +426,28 @@ def test_quantize_paged_hard_values(gpu_device, v, G, n):
     run_quantize(gpu_device, H, D, v, G, E, 16, n, np.arange(n) + 5, -(-(n + 5) // 16), seed=1, x=x, cb=cb)
 
 
+@gpu
+@pytest.mark.parametrize("D,v,G,E", [(64, 8, 8, 100), (64, 8, 1, 256), (64, 8, 1, 16)])
+def test_quantize_paged_most_tokens(gpu_device, D, v, G, E):
+    """2^20 tokens, of which all but a few are padding; each of the kernels."""
+    n, at = 1 << 20, [0, 17, 65535, 65536, 777777, (1 << 20) - 1]
+    rng = np.random.Generator(np.random.PCG64(3))
+    cb = [torch.from_numpy(rng.normal(0, 1, (1, G, E, v)).astype(np.float16)).to(gpu_device) for _ in range(2)]
+    x = torch.zeros((n, 1, D), dtype=torch.float16, device=gpu_device)
+    x[at] = torch.from_numpy(rng.normal(0, 1, (len(at), 1, D)).astype(np.float16)).to(gpu_device)
+    slots = torch.full((n,), -1, dtype=torch.int32, device=gpu_device)
+    slots[at] = torch.arange(20, 20 + len(at), dtype=torch.int32, device=gpu_device)
+    got = []
+    for xs, sl in ((x, slots), (x[at], slots[at])):
+        k = torch.full((4, 1, 16, D // v), 201, dtype=torch.uint8, device=gpu_device)
+        val = torch.full((4, 1, 1, D // v, 16), 201, dtype=torch.uint8, device=gpu_device)
+        vq.vq_kv_quantize_paged(vq.VQKVPagesDev(1, D, v, 16, k, val, *cb), xs, xs, sl)
+        got.append((k, val))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert int((got[0][0] != 201).any(-1).sum()) == len(at)
+
+
 # ------------------------------------------------------------------------------------------------ attention
 
 @gpu
