@@ -26,10 +26,10 @@
 // The rounds of a share are one sequence over all its blocks: codes are requested NB tiles ahead (pages 32 rounds ahead), across blocks too.
 //
 // What bounds it.  Not memory: codes that lie in L2 take as long as codes from HBM (57 and 61 us where both were timed).  Two wavefronts a SIMD, each
-// with a tile's 16 matrix instructions (18 ns each) and 200 vector instructions (1.9 ns: addresses of the gathers, weights), in order: a chunk of 2048 rows
-// by counters has the matrix units busy for 43 % and the vector units for 49 % of the time, 17 % of it together, at 1.9 GHz; no bank conflicts.
+// with a tile's 16 matrix instructions (18 ns each) and 125 vector instructions (1.9 ns: addresses of the gathers, weights), in order: a chunk of 2048 tokens
+// by counters has the matrix units busy for 47 % of the time and issues vector instructions for 46 %, little of it together, at 1.9 GHz; no bank conflicts.
 // A round of 8 tiles takes 1.25 - 1.4 us, and before the first one lie 5 - 6 us: lengths, pages, codebooks, codes, each a trip to memory.
-// 240 GFLOP of a prompt's chunk 0.28 ms (856 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
+// 240 GFLOP of a prompt's chunk 0.27 ms (890 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
 // LDS gathers 1458).  One wavefront a SIMD with 64 rows, where every gather is used twice, took 318 - 365 us: a wavefront alone issues at
 // most one instruction in 4.7 clocks.
 #include "attn_paged.h"
