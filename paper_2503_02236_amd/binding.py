@@ -178,9 +178,9 @@ def _load_marshal(l) -> None:
     address = lambda name: ctypes.cast(getattr(l, name), ctypes.c_void_p).value  # noqa: E731
     native.init(tuple(address(n) for n in ("vq_gemv", "vq_gemv_workspace", "vq_gemv_batch", "vq_gemv_batch_workspace", "vq_gemm",
                                            "vq_gemm_workspace", "vq_attn_decode", "vq_attn_decode_workspace", "vq_kv_quantize")),
-                VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError)
-    native.init_paged(tuple(address(n) for n in ("vq_kv_pages_assign", "vq_kv_quantize_paged", "vq_attn_paged", "vq_attn_paged_workspace")),
-                      VQKVPagesDev, VQPagePlan)
+                VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError,
+                tuple(address(n) for n in ("vq_kv_pages_assign", "vq_kv_quantize_paged", "vq_attn_paged", "vq_attn_paged_workspace")),
+                VQKVPagesDev, VQPagePlan)
     _marshal = native
 
 

@@ -539,10 +539,11 @@ PyObject *attn_paged(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 // (thirteen addresses, VQWeightDev, VQKVDev, vq_gemv_pack_t, VQError, VQKVPagesDev, VQPagePlan)
 PyObject *init(PyObject *, PyObject *args) {
-    unsigned long long a[9];
-    if (!PyArg_ParseTuple(args, "(KKKKKKKKK)OOOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &weight_type, &kv_type, &pack_type, &error_type))
+    unsigned long long a[9], paged[4] = {};   // (without the paged calls' addresses and types these stay what they were)
+    if (!PyArg_ParseTuple(args, "(KKKKKKKKK)OOOO|(KKKK)OO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &weight_type, &kv_type, &pack_type,
+                          &error_type, &paged[0], &paged[1], &paged[2], &paged[3], &pages_type, &plan_type))
         return nullptr;
-    for (PyObject *o : {weight_type, kv_type, pack_type, error_type}) Py_INCREF(o);
+    for (PyObject *o : {weight_type, kv_type, pack_type, error_type, pages_type, plan_type}) Py_XINCREF(o);
     lib.gemv = (decltype(lib.gemv))a[0];
     lib.gemv_workspace = (decltype(lib.gemv_workspace))a[1];
     lib.gemv_batch = (decltype(lib.gemv_batch))a[2];
@@ -552,24 +553,16 @@ PyObject *init(PyObject *, PyObject *args) {
     lib.attn_decode = (decltype(lib.attn_decode))a[6];
     lib.attn_decode_workspace = (decltype(lib.attn_decode_workspace))a[7];
     lib.kv_quantize = (decltype(lib.kv_quantize))a[8];
-    Py_RETURN_NONE;
-}
-
-// the paged calls' addresses and types
-PyObject *init_paged(PyObject *, PyObject *args) {
-    unsigned long long a[4];
-    if (!PyArg_ParseTuple(args, "(KKKK)OO", &a[0], &a[1], &a[2], &a[3], &pages_type, &plan_type)) return nullptr;
-    for (PyObject *o : {pages_type, plan_type}) Py_INCREF(o);
-    lib.kv_pages_assign = (decltype(lib.kv_pages_assign))a[0];
-    lib.kv_quantize_paged = (decltype(lib.kv_quantize_paged))a[1];
-    lib.attn_paged = (decltype(lib.attn_paged))a[2];
-    lib.attn_paged_workspace = (decltype(lib.attn_paged_workspace))a[3];
+    if (!paged[0]) Py_RETURN_NONE;
+    lib.kv_pages_assign = (decltype(lib.kv_pages_assign))paged[0];
+    lib.kv_quantize_paged = (decltype(lib.kv_quantize_paged))paged[1];
+    lib.attn_paged = (decltype(lib.attn_paged))paged[2];
+    lib.attn_paged_workspace = (decltype(lib.attn_paged_workspace))paged[3];
     Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {
     {"init", init, METH_VARARGS, nullptr},
-    {"init_paged", init_paged, METH_VARARGS, nullptr},
     {"gemv", (PyCFunction)(void (*)(void))gemv, METH_FASTCALL, nullptr},
     {"gemv_batch", (PyCFunction)(void (*)(void))gemv_batch, METH_FASTCALL, nullptr},
     {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr},
