@@ -484,7 +484,7 @@ typedef struct vq_paged_batch_t {
     const int *prefix_lens;  /* device, int32 [B]: tokens that every new token attends; or NULL (= 0) */
     const float *slopes;     /* device, fp32 [Hq], or NULL */
     int window;              /* tokens that a new token looks back on, itself among them; 0: all */
-    float softcap;           /* 0: none */
+    float softcap;           /* 0: none; otherwise of any finite size */
 } vq_paged_batch_t;
 int vq_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *batch, const void *q, size_t q_stride, float sm_scale,
                   void *out, size_t out_stride, void *ws, size_t ws_bytes, void *stream);

@@ -32,6 +32,8 @@
 // 240 GFLOP of a prompt's chunk 0.27 ms (890 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
 // LDS gathers 1458).  One wavefront a SIMD with 64 rows, where every gather is used twice, took 318 - 365 us: a wavefront alone issues at
 // most one instruction in 4.7 clocks.
+#include <algorithm>
+
 #include "attn_paged.h"
 
 namespace vq {
@@ -225,9 +227,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     }
                 }
                 if constexpr (MODS) {   // (two uniform branches: a choice per score would compute both sides)
-                    if (a.cap_out > 0.f) {
+                    if (a.cap_in > 0.f) {
+                        if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
+                            const int see = attended_keys(t0 + 16 * lh, see_from, see_to, pc.prefix);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) s[e] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f);
+                            for (int e = 0; e < 16; ++e) s[e] = attended_or_zero(s[e], see, 4 * (e & 3) + (e >> 2));
+                        }
+                        cap_scores(a, scale2, [&](int e) { return s[e]; }, [&](int e, float x) { s[e] = x; });
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s[e] *= scale2;
@@ -499,7 +505,7 @@ int run_wide(const PagedArgs &a, hipStream_t s) {
 }
 template <int D, int V>
 int run_paged_as(const PagedArgs &a, hipStream_t s) {
-    const bool mods = a.cap_out > 0.f || a.slopes;
+    const bool mods = a.cap_in > 0.f || a.slopes;
     if (a.G == 1) return mods ? run_wide<D, V, true, true>(a, s) : run_wide<D, V, true, false>(a, s);
     return mods ? run_wide<D, V, false, true>(a, s) : run_wide<D, V, false, false>(a, s);
 }
@@ -554,8 +560,10 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     const float scale = sm_scale < 0.f ? -sm_scale : sm_scale;
     a.scale2 = scale * kLog2e > FLT_MIN ? scale * kLog2e : FLT_MIN;   // (above zero: minus infinity times it has to stay)
     a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;
-    a.cap_out = b->softcap * kLog2e;
-    a.cap_in = b->softcap > 0.f ? 2.f * a.scale2 / b->softcap : 0.f;
+    // (finite: a zero score times the first stays zero, and a cap that the second shortens is beyond any score)
+    a.cap_in = b->softcap > 0.f ? std::min(2.f * a.scale2 / b->softcap, FLT_MAX) : 0.f;
+    a.cap_out = std::min(b->softcap * kLog2e, FLT_MAX / 4);
+    for (int i = 0; i < 3; ++i) a.cap_poly[i] = kCapPoly[i] * a.scale2;
     if (p.few) return launch_few(a, kv->v, s);
     if (kv->D == 64) return kv->v == 8 ? run_paged_as<64, 8>(a, s) : kv->v == 4 ? run_paged_as<64, 4>(a, s) : run_paged_as<64, 2>(a, s);
     return kv->v == 8 ? run_paged_as<128, 8>(a, s) : kv->v == 4 ? run_paged_as<128, 4>(a, s) : run_paged_as<128, 2>(a, s);

@@ -169,10 +169,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             auto body = [&](int tile, Codes &codes, const Codes &after, const Codes &second) {
                 const int idx = idx0 + (tile << 3), t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * KEYS;
                 if constexpr (MODS) {
-                    if (a.cap_out > 0.f) {
+                    if (a.cap_in > 0.f) {
+                        if (__builtin_expect((unsigned)(t0 - all_from) > all_span, 0)) {
+                            const int see = attended_keys(t0 + 16 * g, see_from, see_to, pc.prefix);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            s[e / 4][e % 4] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e / 4][e % 4] * a.cap_in) + 1.f);
+                            for (int e = 0; e < 16; ++e) s[e / 4][e % 4] = attended_or_zero(s[e / 4][e % 4], see, 4 * (e % 4) + e / 4);
+                        }
+                        cap_scores(a, scale2, [&](int e) { return s[e / 4][e % 4]; }, [&](int e, float x) { s[e / 4][e % 4] = x; });
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s[e / 4][e % 4] *= scale2;
@@ -356,7 +359,7 @@ int run_few(const PagedArgs &a, hipStream_t s) {
 }
 template <int V>
 int run_few_as(const PagedArgs &a, hipStream_t s) {
-    const bool mods = a.cap_out > 0.f || a.slopes;
+    const bool mods = a.cap_in > 0.f || a.slopes;
     if (a.G == 1) return mods ? run_few<V, true, true>(a, s) : run_few<V, true, false>(a, s);
     return mods ? run_few<V, false, true>(a, s) : run_few<V, false, false>(a, s);
 }

@@ -1,0 +1,76 @@
+"""Scores of vq_attn_paged where they are hard on the arithmetic: caps of any size."""
+import numpy as np
+import pytest
+import torch
+
+import paged_reference
+from test_paged import Case, attend, on_a_wide_table
+
+gpu = pytest.mark.gpu
+KERNELS = [dict(v=4), dict(v=2, G=64), dict(v=8, D=64), dict(v=4, G=1, wide=True), dict(v=8, G=8, wide=True)]     # wide: tiles of few rows
+REQS = [(120, 23), (17, 0), (700, 1), (64, 3), (3, 8), (0, 0)]
+
+
+def make(reqs, wide=False, **kw):
+    case = Case(reqs, **{**dict(H=2, group=2), **kw})
+    return on_a_wide_table(case) if wide else case
+
+
+# ------------------------------------------------------------------------------------------------ caps
+
+def test_the_capped_reference_is_the_cap_itself():
+    """The bound of a capped score by an fp32 emulation of the two forms, and against caps that are none."""
+    rng = np.random.Generator(np.random.PCG64(1))
+    case = Case([(40, 40)], H=1, softcap=1e30, seed=1)
+    free = Case([(40, 40)], H=1, seed=1)
+    a, ba = paged_reference.attend(case)
+    b, bb = paged_reference.attend(free)
+    assert np.abs(a - b).max() <= 1e-12 and (ba <= bb + 1e-5).all()
+    f = np.float32
+    for cap in (1e-3, 3.0, 30.0, 1e4, 1e6, 3e38):
+        s = rng.normal(0, 2, 4096).astype(np.float32)
+        x = s * f(min(2 * 1.4426950408889634 / cap, np.finfo(np.float32).max))
+        w = x * x
+        scale = f(0.7)                                     # (of the scores, in the polynomial's coefficients)
+        c = [f(k) * scale for k in (-4.00369909e-02, 1.91897040e-03, -8.53218143e-05)]
+        small = s * (w * (w * (w * c[2] + c[1]) + c[0]) + scale) / scale
+        with np.errstate(over="ignore"):
+            large = f(cap) - f(2) * (f(cap) / (np.exp2(x) + f(1)))
+        got = np.where(np.abs(x).max() <= 1, small, large).astype(np.float64)
+        want = cap * np.tanh(s.astype(np.float64) / cap)
+        top = np.abs(s).max()
+        allowed = 6 * 2.0 ** -24 * np.abs(want) + (0 if 2.885 * top < 0.999 * cap else 14 * 2.0 ** -24 * min(cap, 2.9 * top))
+        assert (np.abs(got - want) <= allowed).all(), cap
+
+
+@gpu
+@pytest.mark.parametrize("softcap", [1e-42, 1e-30, 0.01, 3.0, 50.0, 1e4, 1e6, 1e8, 1.2e38, 3.0e38, float(np.finfo(np.float32).max)])
+@pytest.mark.parametrize("kw", KERNELS)
+def test_a_cap_of_any_size(gpu_device, softcap, kw):
+    """A large cap is none, a small one leaves equal scores; zero scores stay zero under both."""
+    case = make(REQS, seed=3, softcap=softcap, sigma=2.0, extra_rows=2, **kw)
+    case.q[2] = 0
+    paged_reference.check(case, attend(case, gpu_device))
+
+
+@gpu
+@pytest.mark.parametrize("softcap", [2.0, 40.0, 1e5])
+@pytest.mark.parametrize("kw", KERNELS)
+@pytest.mark.parametrize("mods", [dict(window=20, prefix=[5, 0, 300, 40, 0, 1]), dict(slopes=[0.5, 0.01, 2.0, -0.02], prefix=[90, 9, 2, 64, 0, 65], window=17), dict(sm_scale=-0.6), dict(sm_scale=0.0)])
+def test_caps_with_masks_and_biases(gpu_device, softcap, kw, mods):
+    case = make(REQS, seed=4, softcap=softcap, sigma=3.0, extra_rows=1, **kw, **mods)
+    paged_reference.check(case, attend(case, gpu_device))
+
+
+@gpu
+@pytest.mark.parametrize("softcap", [2.0, 40.0])
+@pytest.mark.parametrize("kw", KERNELS)
+def test_capped_rows_ignore_what_they_do_not_attend(gpu_device, softcap, kw):
+    """Codes behind a request's end that name large or infinite entries: the very same bits."""
+    case = make([(37, 5), (100, 1), (16, 2), (31, 3)], E=199, seed=13, softcap=softcap, **kw)
+    base = attend(case, gpu_device)
+    k_cb, v_cb = case.k_cb, case.v_cb
+    for value in (300.0, np.inf, np.nan):
+        more = np.full(k_cb.shape[:2] + (57, case.v), value, np.float16)
+        case.k_cb, case.v_cb = np.concatenate([k_cb, more], 2), np.concatenate([v_cb, more], 2)
+        assert torch.equal(attend(case, gpu_device), base), value
