@@ -11,7 +11,7 @@
 //                 the transposing LDS read hands them out by channel; for v = 2 a lane reads its channels' pairs for the block's
 //                 tokens and permutes them into operands.
 // A weight is 2^(s - m + 6) rounded to a half (relative error 2^-11, what the matrix instruction takes; the sum l adds the rounded ones, so
-// that weights add up to one): m follows the maximum only when that has grown by more than 8, so weights lie below 2^14 and those
+// that weights add up to one): m follows the row's own maximum, and only when that has grown by more than 8, so weights lie below 2^14 and those
 // that fall below a half's range are below 2^-31 of the largest.  Sums, statistics and outputs before the last rounding are fp32.
 //
 // Codebooks in LDS (64 KiB a side).  One codebook per head: every entry 256 / (2 v) times in a row of 256 bytes, lane l reads copy l, and no
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
                 if (!MODS) mt *= scale2;
                 if (__ballot(mt > m_ref + kRise)) {
-                    const float m_new = mt > m_ref ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                    const float m_new = mt > m_ref + kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
                     lsum *= f;
 #pragma unroll

@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                 }
                 if (!MODS) mt *= scale2;
                 if (__builtin_expect(__ballot(mt > m_ref + kRise) != 0, 0)) {
-                    const float m_new = mt > m_ref ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                    const float m_new = mt > m_ref + kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
                     lsum *= f;
 #pragma unroll

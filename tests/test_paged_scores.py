@@ -1,4 +1,4 @@
-"""Scores of vq_attn_paged where they are hard on the arithmetic: caps of any size."""
+"""Scores of vq_attn_paged where they are hard on the arithmetic: caps of any size, rows beside others."""
 import numpy as np
 import pytest
 import torch
@@ -74,3 +74,27 @@ def test_capped_rows_ignore_what_they_do_not_attend(gpu_device, softcap, kw):
         more = np.full(k_cb.shape[:2] + (57, case.v), value, np.float16)
         case.k_cb, case.v_cb = np.concatenate([k_cb, more], 2), np.concatenate([v_cb, more], 2)
         assert torch.equal(attend(case, gpu_device), base), value
+
+
+# ------------------------------------------------------------------------------------------------ rows and their neighbours
+
+@gpu
+@pytest.mark.parametrize("mods", [dict(), dict(softcap=30.0), dict(slopes=[0.0, 0.01, 0.0, 0.02])])
+@pytest.mark.parametrize("kw", KERNELS)
+def test_a_row_does_not_depend_on_its_neighbours_queries(gpu_device, kw, mods):
+    """Every other row's query changes, to one whose scores grow from tile to tile and to ones of other sizes: the rest keep every bit."""
+    case = make([(1501, 13), (90, 3)], v=kw["v"], **{k: x for k, x in kw.items() if k != "v"}, seed=6, **mods)
+    order = np.argsort(case.values(case.K_codes[0], case.k_cb)[:, 0] @ case.q[0, 0].astype(np.float64))
+    case.K_codes[0] = case.K_codes[0][order]
+    t = np.arange(1501)
+    case.k_codes[case.table[0, t // 16], :, t % 16] = case.K_codes[0]
+    q = case.q.copy()
+    base = attend(case, gpu_device)
+    paged_reference.check(case, base)
+    direction = q[0, 0].astype(np.float32)
+    for scale in (0.0, 1.5, 6.0):
+        for odd in (0, 1):
+            case.q = q.copy()
+            rows = case.q[odd::2]
+            rows[:] = (direction * scale).astype(np.float16)
+            assert torch.equal(attend(case, gpu_device)[1 - odd::2], base[1 - odd::2]), (scale, odd)
