@@ -20,7 +20,13 @@ constexpr int kScanOff = kStatOff + 2048;
 constexpr int kListOff = kScanOff + 256;      // pieces of the share, 64 at a time: their first rounds, and a Piece each
 constexpr int kBaseOff = kListOff + 256 + 64 * 64;   // where the codes of the next rounds lie, [wave][64]
 constexpr int kLds = kBaseOff + kWaves * 64 * 8;
-constexpr float kHeadroom = 6.f, kRise = 8.f; // (log2)
+// Weights are 2^(s - m + 6), s up to 6 above m.  6 - m is a float: off by 2 at most upwards (where m's last bit is worth 4 or 8, from 2^25 on; beyond, it is
+// -m), so a weight is 2^14 at most, a half, whatever the scores.
+constexpr float kHeadroom = 6.f, kRise = 6.f; // (log2)
+// s is a product that the weight's fused multiply-add does not round, and the maximum does: beyond this they may differ by as much as a weight's
+// rounding and more (from 2^25 on weights would be no halves), so such rows' scores are rounded and taken less m first.
+constexpr float kFar = 1048576.f;
+__device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && m != -FLT_MAX; }
 
 struct PagedArgs {
     const uint8_t *k_codes, *v_codes;

@@ -11,7 +11,7 @@
 //                 the transposing LDS read hands them out by channel; for v = 2 a lane reads its channels' pairs for the block's
 //                 tokens and permutes them into operands.
 // A weight is 2^(s - m + 6) rounded to a half (relative error 2^-11, what the matrix instruction takes; the sum l adds the rounded ones, so
-// that weights add up to one): m follows the row's own maximum, and only when that has grown by more than 8, so weights lie below 2^14 and those
+// that weights add up to one): m follows the row's own maximum, and only when that has grown by more than 6, so weights lie below 2^12 and those
 // that fall below a half's range are below 2^-31 of the largest.  Sums, statistics and outputs before the last rounding are fp32.
 //
 // Codebooks in LDS (64 KiB a side).  One codebook per head: every entry 256 / (2 v) times in a row of 256 bytes, lane l reads copy l, and no
@@ -182,6 +182,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
             float m_ref = -FLT_MAX, lsum = 0.f;
+            bool far = false;   // a reference of the wavefront is
             // tiles of this wavefront's rows, of those of the block
             const int pos_f = pc.pos0 + token_of(a, max(row0, 0)), pos_l = pc.pos0 + token_of(a, max(row0 + tile_rows - 1, 0));
             const int count = tile_rows > 0 ? min(pc.front + max(((max(pos_l + 1, pc.prefix) + 31) >> 5) - pc.lo, 0), pc.count) : 0;
@@ -258,16 +259,28 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     mt = __builtin_elementwise_maximum(__uint_as_float(y[0]), __uint_as_float(y[1]));
                 }
                 if (!MODS) mt *= scale2;
-                if (__ballot(mt > m_ref + kRise)) {
-                    const float m_new = mt > m_ref + kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                if (__ballot(mt - m_ref > kRise)) {
+                    const float m_new = mt - m_ref > kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
+                    if (!MODS) far = __ballot(is_far(m_ref)) != 0;
                     lsum *= f;
 #pragma unroll
                     for (int k = 0; k < CH; ++k)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[k][e] *= f;
                 }
-                const float sub = kHeadroom - m_ref;
+                float sub = kHeadroom - m_ref;
+                if (__builtin_expect(!MODS && far, 0)) {
+                    const bool mine = is_far(m_ref);
+                    const float back = __builtin_amdgcn_rcpf(scale2);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float x = s[e] * scale2;
+                        asm("" : "+v"(x));   // (rounded, as the maximum is)
+                        s[e] = mine ? (x - m_ref) * back : s[e];
+                    }
+                    sub = mine ? kHeadroom : sub;
+                }
 
                 // Values of 16 keys, k of the two steps: operands as they come (TR), or channel pairs of the lane's eight keys.
                 // TR: lane 4 e + c of a group of 16 asks for the entry of key 16 lh + 4 e + 2 k + j and position block c, part f; the

@@ -141,6 +141,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
             for (int f = 0; f < F; ++f) o[f] = float4_t{0.f, 0.f, 0.f, 0.f};
             float m_ref = -FLT_MAX, lsum = 0.f;
+            bool far = false;   // a reference of the wavefront is
             // this wavefront's tiles: idx0, idx0 + 8, ...
             const int pos_f = pc.pos0 + token_of(a, pc.row0), pos_l = pc.pos0 + token_of(a, pc.row0 + rows - 1);
             const int idx0 = (pc.r0 << 3) + wave, rounds = pc.r1 - pc.r0;
@@ -213,14 +214,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     mt = __builtin_elementwise_maximum(__uint_as_float(z[0]), __uint_as_float(z[1]));
                 }
                 if (!MODS) mt *= scale2;
-                if (__builtin_expect(__ballot(mt > m_ref + kRise) != 0, 0)) {
-                    const float m_new = mt > m_ref + kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
+                if (__builtin_expect(__ballot(mt - m_ref > kRise) != 0, 0)) {
+                    const float m_new = mt - m_ref > kRise ? mt : m_ref, f = __builtin_amdgcn_exp2f(m_ref - m_new);
                     m_ref = m_new;
+                    if (!MODS) far = __ballot(is_far(m_ref)) != 0;
                     lsum *= f;
 #pragma unroll
                     for (int k = 0; k < F; ++k) o[k] *= f;
                 }
-                const float sub = kHeadroom - m_ref;
+                float sub = kHeadroom - m_ref;
+                if (__builtin_expect(!MODS && far, 0)) {
+                    const bool mine = is_far(m_ref);
+                    const float back = __builtin_amdgcn_rcpf(scale2);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float x = s[e / 4][e % 4] * scale2;
+                        asm("" : "+v"(x));   // (rounded, as the maximum is)
+                        s[e / 4][e % 4] = mine ? (x - m_ref) * back : s[e / 4][e % 4];
+                    }
+                    sub = mine ? kHeadroom : sub;
+                }
                 V16 vop[2][F];
                 auto gather_v = [&](int k, int at) {   // step k, part f of the position block, half j of the four keys
                     const int f = at / 2, j = at % 2, n = f * 4 / V;

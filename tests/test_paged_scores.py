@@ -1,4 +1,4 @@
-"""Scores of vq_attn_paged where they are hard on the arithmetic: caps of any size, rows beside others."""
+"""Scores of vq_attn_paged where they are hard on the arithmetic: caps of any size, rows beside others, scores of millions, very many small weights."""
 import numpy as np
 import pytest
 import torch
@@ -98,3 +98,64 @@ def test_a_row_does_not_depend_on_its_neighbours_queries(gpu_device, kw, mods):
             rows = case.q[odd::2]
             rows[:] = (direction * scale).astype(np.float16)
             assert torch.equal(attend(case, gpu_device)[1 - odd::2], base[1 - odd::2]), (scale, odd)
+
+
+# ------------------------------------------------------------------------------------------------ large scores, small weights
+
+def exact_case(kw, n, level, seed):
+    """Scores that are whole multiples of `level`: the queries are one in one channel, the entries multiples of level there and zero elsewhere."""
+    case = make([(n, 3), (70, 1)], seed=seed, **kw)
+    case.q[:] = 0
+    case.q[:, :, 0] = 1024
+    rng = np.random.Generator(np.random.PCG64(seed))
+    case.k_cb[:] = 0
+    case.k_cb[..., 0] = rng.integers(-8, 9, case.k_cb.shape[:3]) * level
+    case.k_cb[:, :, 0, 0] = 8 * level
+    case.sm_scale = 1.0
+    return case
+
+
+@gpu
+@pytest.mark.parametrize("kw", KERNELS)
+@pytest.mark.parametrize("level", [2.0 ** 7, 2.0 ** 10, 2.0 ** 12])
+@pytest.mark.parametrize("sm_scale", [1.0, 0.7, 30.0, -0.7])
+@pytest.mark.parametrize("softcap", [0.0, 1e30])
+def test_scores_of_millions_and_more(gpu_device, kw, level, sm_scale, softcap):
+    """Finite inputs give finite outputs: the keys of the largest score share the weight, the others, far below, have none."""
+    case = exact_case(kw, 900, level, 5)
+    case.sm_scale, case.softcap = sm_scale, softcap
+    got = attend(case, gpu_device).float().cpu().numpy().astype(np.float64)
+    for b, (ln, n) in enumerate(case.reqs):
+        K, V = case.values(case.K_codes[b], case.k_cb), case.values(case.V_codes[b], case.v_cb)
+        for i in range(n):
+            for hq in range(case.H * case.group):
+                s = sm_scale * K[:ln - n + i + 1, hq // case.group, 0]
+                top = s == s.max()
+                val = V[:ln - n + i + 1, hq // case.group][top]
+                # every weight is the same half, so their rounding cancels: the sum of products, its parts and the output are rounded
+                bound = 2.0 ** -11 * np.abs(val.mean(0)) + (len(val) + 8) * 2.0 ** -24 * np.abs(val).mean(0) + 2.0 ** -25
+                assert (np.abs(got[case.cu[b] + i, hq] - val.mean(0)) <= bound).all(), (b, i, hq)
+
+
+@gpu
+@pytest.mark.parametrize("kw", KERNELS)
+@pytest.mark.parametrize("bits", [19.0, 21.5, 24.25, 27.5])
+@pytest.mark.parametrize("first", [True, False])
+def test_many_small_weights_beside_a_large_one(gpu_device, kw, bits, first):
+    """One key of weight 1 and thousands of 2^-bits: as halves those are subnormal, and together they count."""
+    n = 20000
+    case = make([(n, 1)], **{**dict(H=1, group=1), **kw}, E=2, seed=8)
+    P = case.D // case.v
+    case.q[:] = 1
+    case.k_cb[:] = 0
+    case.k_cb[:, :, 1] = 0.25
+    case.v_cb[:] = -30.0
+    case.v_cb[:, :, 1] = 1.0
+    case.sm_scale = bits * np.log(2) / (0.25 * case.D)
+    one = np.zeros((n, 1, P), np.uint8)
+    one[0 if first else n - 1] = 1
+    case.K_codes = case.V_codes = [one]
+    t = np.arange(n)
+    case.k_codes[case.table[0, t // 16], :, t % 16] = one
+    case.v_codes[case.table[0, t // 16], :, t % 16 // 16, :, t % 16] = one
+    paged_reference.check(case, attend(case, gpu_device))
