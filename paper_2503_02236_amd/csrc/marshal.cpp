@@ -95,7 +95,7 @@ void *data(PyObject *o, at::ScalarType type) {
     return t.data_ptr();
 }
 
-// No mode that would see the allocation of an output.
+// No mode that would see the allocation of an output or the reading of a tensor.
 void no_modes() {
     const auto on = c10::impl::tls_local_dispatch_key_set().included_;
     if (at::impl::PythonTorchFunctionTLS::stack_len() > 0 || on.has(c10::DispatchKey::Python) || on.has(c10::DispatchKey::PythonTLSSnapshot) ||
@@ -432,6 +432,7 @@ PyObject *kv_quantize(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyObject *kv_pages_assign(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return guarded([&]() -> PyObject * {
         if (n != 8 || (PyObject *)Py_TYPE(args[6]) != plan_type) throw NotPlain();
+        no_modes();
         const at::Tensor &table = tensor(args[2]), &lens = tensor(args[0]), &free_pages = tensor(args[3]);   // (on a GPU, so that there is a stream)
         const auto current = c10::hip::getCurrentHIPStream();
         const int device = current.device_index();
@@ -473,6 +474,7 @@ PyObject *kv_pages_assign(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyObject *kv_quantize_paged(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return guarded([&]() -> PyObject * {
         if (n != 4) throw NotPlain();
+        no_modes();
         strided_tensor(args[1]);   // (on a GPU, so that there is a stream)
         const auto current = c10::hip::getCurrentHIPStream();
         const int device = current.device_index();
