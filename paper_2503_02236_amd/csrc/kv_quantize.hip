@@ -749,20 +749,26 @@ int run_kvq(KvQuantArgs &a, int bh, hipStream_t s) {
 
 }  // namespace
 
-// What a call does (for tests): kernel, its variant (matrix cores), tokens per workgroup, threads, workgroups that share a token range.
-void kv_quantize_plan_of(const vq_kv_t *kv, int n_new, int out[5]) {
-    const int bh = kv->B * kv->H, P = kv->D / kv->v;
-    out[0] = kv_quantize_kernel_of(kv, n_new);
-    out[1] = 0;
-    out[2] = std::min(n_new, out[0] == kKvqScan ? kQuantScanTokens : kQuantLaneTokens);
+// What a call does (for tests): kernel, its variant (matrix cores) or tokens at a time (lanes), tokens per workgroup, threads, workgroups that share a token range.
+static void kvq_plan_of(int bh, int P, int v, int E, int G, int n_new, int *scan_tokens, int out[5]) {
+    out[0] = kvq_choice(bh, P, v, E, G, n_new, scan_tokens);
+    out[1] = out[0] == kKvqLane && scan_tokens && kvq_four_tokens(P, v, n_new) ? 4 : 0;
+    out[2] = std::min(n_new, out[0] == kKvqLane ? kQuantLaneTokens : scan_tokens ? *scan_tokens : kQuantScanTokens);
     out[3] = out[0] == kKvqScan ? 512 : 256;
     out[4] = out[0] == kKvqScan ? kvq_share(bh, ceil_div(n_new, out[2]), out[2] * P) : 1;
     if (out[0] == kKvqMfma) {
-        const KvqMfmaPlan p = kvq_mfma_plan(bh, P, kv->v, kv->n_entries, kv->cb_groups, n_new);
+        const KvqMfmaPlan p = kvq_mfma_plan(bh, P, v, E, G, n_new);
         out[1] = p.way;
         out[2] = p.tokens;
         out[3] = p.threads;
     }
+}
+void kv_quantize_plan_of(const vq_kv_t *kv, int n_new, int out[5]) {
+    kvq_plan_of(kv->B * kv->H, kv->D / kv->v, kv->v, kv->n_entries, kv->cb_groups, n_new, nullptr, out);
+}
+void kv_quantize_paged_plan_of(const vq_kv_pages_t *kv, int n_tokens, int out[5]) {
+    int scan_tokens = kQuantScanTokens;
+    kvq_plan_of(kv->H, kv->D / kv->v, kv->v, kv->n_entries, kv->cb_groups, n_tokens, &scan_tokens, out);
 }
 
 int launch_kv_quantize(const vq_kv_t *kv, const void *k_new, const void *v_new, int n_new, int pos, hipStream_t s) {
