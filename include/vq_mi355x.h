@@ -412,7 +412,8 @@ typedef struct vq_kv_pages_t {
  *      first), in order of b, and written to the table behind those it has.
  *   A request is refused (status[b] = 1: no tokens, no pages, length as it was) if its tokens would not fit the table's row,
  *   if the new tokens of the requests up to it (those that fit their row, refused or not) pass n_tokens, or if it needs pages and
- *   those needed up to it (by requests not refused for the other reasons) pass the pool.  status[b] is 0 otherwise.
+ *   those needed up to it (by requests not refused for the other reasons) pass the pool.  status[b] is 0 otherwise.  So one request that asks for more
+ *   than the step or the pool has holds up those with new tokens (new pages) behind it: ask for a long prompt in chunks that fit.
  * Reads lens, new_lens, n_free, free_pages [0, n_free), block_table; writes everything else below.  With seq_lens and n_free_out apart
  * from lens and n_free a call may be made again with the same result as long as nobody else changed the arrays; with the same arrays it steps in place.
  * Table entries behind a request's pages, and free_pages behind the pool's end, are left as they are.
@@ -445,7 +446,8 @@ int vq_kv_pages_assign(const vq_page_step_t *step, void *stream);
  * written to their slots.
  *   k_new, v_new: device fp16, token i's head h at element i * stride + h * D (k_stride, v_stride >= H * D, multiples of 8, at most
  *   2^23: the tensors may be parts of a fused projection's output).
- *   slots: device int32 [n_tokens]; a slot outside [0, n_pages * page_tokens) is skipped (padding).  Slots that are written must differ.
+ *   slots: device int32 [n_tokens]; a slot outside [0, n_pages * page_tokens) is skipped (padding): nothing is written for it, but a token costs
+ *   its time whatever its slot.  Slots that are written must differ.
  *   0 <= n_tokens <= 2^20.
  * Codebooks of one side of a head must fit 64 KiB, (G * E * v) % 8 == 0 (VQ_ERR_UNSUPPORTED otherwise).
  */
@@ -461,6 +463,8 @@ int vq_kv_quantize_paged(const vq_kv_pages_t *kv, const void *k_new, size_t k_st
  *   slopes:        s(t) = s(t) - slopes[hq] * |pos - t|
  *   visible(t) = t < seq_lens[b] and ( t <= pos and (window == 0 or t > pos - window)  or  t < prefix_lens[b] )
  *   out     = softmax over the visible t of s(t) . V[b][h][t]; zeros where nothing is visible
+ * Scores, statistics and sums are fp32; a weight of the softmax is rounded to fp16 (relative error 2^-11) for the product with V, and the sum
+ * of weights adds the rounded ones: an output is off by up to 2^-10 of the attended values' weighted sizes beside its own rounding.
  * Rows of q and out behind cu_new[B] are neither read nor written.
  *   q, out: device fp16, token i's head hq at element i * stride + hq * D (strides >= Hq * D, multiples of 8); they must not overlap.
  * Tokens that a row does not attend never matter, with whatever codes behind a request's length; entries that codes of

@@ -655,7 +655,9 @@ def vq_kv_pages_assign(new_lens: torch.Tensor, lens: torch.Tensor, block_table: 
                        page_tokens: int, n_tokens: Optional[int] = None, plan: Optional[VQPagePlan] = None,
                        n_free_out: Optional[torch.Tensor] = None) -> VQPagePlan:
     """Pages for the new tokens of every request, and the pages of ended ones back: updates block_table, free_pages and
-    ``n_free_out`` (``n_free`` itself unless given), fills and returns ``plan`` (for ``n_tokens`` new tokens at most)."""
+    ``n_free_out`` (``n_free`` itself unless given), fills and returns ``plan`` (for ``n_tokens`` new tokens at most).  ``plan.status`` is 1 for a
+    request that got nothing; one that asks for more than the step or the pool has is among them and holds up the requests behind it, so ask for
+    a long prompt in chunks."""
     if _marshal is not None and plan is not None:
         r = _marshal.kv_pages_assign(new_lens, lens, block_table, free_pages, n_free, page_tokens, plan, n_free_out)
         if r is not NotImplemented:
@@ -680,7 +682,8 @@ def vq_kv_pages_assign(new_lens: torch.Tensor, lens: torch.Tensor, block_table: 
 
 
 def vq_kv_quantize_paged(kv: VQKVPagesDev, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
-    """Quantize new tokens (fp16 [tokens][H][D] each, tokens may lie apart) and store their codes at their slots (negative: skipped)."""
+    """Quantize new tokens (fp16 [tokens][H][D] each, tokens may lie apart) and store their codes at their slots.  A negative slot
+    is skipped, though its token takes its time all the same."""
     if _marshal is not None and _marshal.kv_quantize_paged(kv, k_new, v_new, slots) is not NotImplemented:
         return
     d = kv.desc()
@@ -703,7 +706,8 @@ def vq_attn_paged(kv: VQKVPagesDev, q: torch.Tensor, sm_scale: float, block_tabl
                   out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, window: int = 0, softcap: float = 0.0,
                   slopes: Optional[torch.Tensor] = None, prefix_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[tokens][Hq][D]: attention of every request's new tokens (q, fp16, tokens may lie apart) over its pages, causal, optionally with
-    a sliding ``window``, capped scores, a distance bias and a prefix that all of them attend."""
+    a sliding ``window``, capped scores, a distance bias and a prefix that all of them attend.  Rows of ``out`` behind the last request's new
+    tokens are left as they are: without an ``out`` they hold whatever the new tensor held."""
     if _marshal is not None:
         r = _marshal.attn_paged(kv, q, sm_scale, block_table, cu_new, seq_lens, out, ws, window, softcap, slopes, prefix_lens)
         if r is not NotImplemented:

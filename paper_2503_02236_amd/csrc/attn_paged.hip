@@ -27,9 +27,9 @@
 //
 // What bounds it.  Not memory: codes that lie in L2 take as long as codes from HBM (57 and 61 us where both were timed).  Two wavefronts a SIMD, each
 // with a tile's 16 matrix instructions (18 ns each) and 125 vector instructions (1.9 ns: addresses of the gathers, weights), in order: a chunk of 2048 tokens
-// by counters has the matrix units busy for 47 % of the time and issues vector instructions for 46 %, little of it together, at 1.9 GHz; no bank conflicts.
+// by counters has the matrix units busy for 46 % of the time and issues vector instructions for 45 %, little of it together, at 1.9 GHz; no bank conflicts.
 // A round of 8 tiles takes 1.25 - 1.4 us, and before the first one lie 5 - 6 us: lengths, pages, codebooks, codes, each a trip to memory.
-// 240 GFLOP of a prompt's chunk 0.27 ms (890 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
+// 240 GFLOP of a prompt's chunk 0.27 - 0.29 ms by machine (823 - 900 TFLOP/s; a register loop of the same instruction reaches 1645 with such operands, fed by
 // LDS gathers 1458).  One wavefront a SIMD with 64 rows, where every gather is used twice, took 318 - 365 us: a wavefront alone issues at
 // most one instruction in 4.7 clocks.
 #include <algorithm>
@@ -494,7 +494,8 @@ PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     // one of 32 rows and 32 keys, so long caches take less (us of both, few rows first; H = 32, a row a request: 16 requests of 16384 tokens
     // 132 and 150, 64 of 4096 154 and 165; H = 8, 16 rows a request: 64 of 16384 125 and 163, 64 of 1024 32 and 44), but a
     // wavefront alone with a larger tile is later with it (one of 300 tokens 17 and 13, H = 32; 16 of 2048 42 and 38).  The wider
-    // tiles take longer per row beyond four (their sums join in more steps), so there it pays earlier.
+    // tiles take longer per row beyond four (their sums join in more steps), so there it pays earlier.  The average is all that the host knows: a
+    // chunk among many single tokens runs in such tiles too.  D = 64 and v = 2 have no such tile, built or timed.
     const long long keys = (long long)b->B * kv->H * b->max_pages * kv->page_tokens, few_rows = (long long)b->n_tokens * (b->Hq / kv->H);
     p.few = few_supported(kv->D, kv->v) && few_rows <= 16ll * b->B && keys >= (few_rows > 4ll * b->B ? 1ll << 18 : 1ll << 21);
     // Wavefronts that share rows read other tiles of keys and join their sums; wavefronts with rows of their own gather the same keys each, and few
@@ -502,8 +503,8 @@ PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     // 102400 225 / 238 / 245, 268800 329 / 370 / 474.
     p.min_log_ways = p.few ? 3 : rows >= 96 * 1024 ? 0 : rows >= 40 * 1024 ? 1 : 2;
     // Blocks of short requests stay whole: a share's border inside one costs the joining launch, 2 - 5 us, more than the shares' evenness gains.  Whole and
-    // cut, us: 8 requests of 1000 tokens, a new one each, 16.6 and 23.2; 4 of 900 new tokens of 1000, 96 and 108; of 1500 60 and 63; 8 of 2000 19.8 and 24.0, but
-    // 16 of 500 new ones of 2000 268 and 260.
+    // cut, us: 8 requests of 1000 tokens, a new one each, 16.6 and 23.2; 4 of 900 new tokens of 1000, 96 and 108; of 1500 60 and 63.  At 2000 chunks gain by the
+    // cut (16 of 500 new ones 268 and 260) and a few single tokens lose (8 of them 19.8 and 24.0): the line looks at lengths alone and takes the chunks' side.
     p.cut = p.workers > 1 && (long long)b->max_pages * kv->page_tokens > 1536;
     p.ws = p.cut ? (size_t)kv->H * p.workers * 2 * ((kWaves * (p.few ? 16 : 32)) >> p.min_log_ways) * (kv->D + 2) * sizeof(float) : 0;
     return p;

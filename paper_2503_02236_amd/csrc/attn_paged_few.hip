@@ -9,7 +9,7 @@
 //                 the transposing read hands them out by channel.
 // D = 128, v = 4 or 8.  A round of 8 tiles takes 1.6 us, of twice the keys that the wider tiles take 1.3 us for.  What is left is what a tile costs whatever its
 // rows: a gather and its address for every 8 bytes of entries (64 of each in 115 vector instructions), and the time until all wavefronts are done with a
-// request (2 - 4 us, its sums 1 us).  16 requests of up to 4096 tokens, 32 heads: 48 us, where their 103 MB of codes would take 15 from HBM.
+// request (2 - 4 us, its sums 1 us).  16 requests of up to 4096 tokens, 32 heads: 48.2 us, where their 103 MB of codes would take 15 from HBM.
 #include "attn_paged.h"
 
 namespace vq {
