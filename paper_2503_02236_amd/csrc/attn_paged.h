@@ -23,8 +23,8 @@ constexpr int kLds = kBaseOff + kWaves * 64 * 8;
 // Weights are 2^(s - m + 6), s up to 6 above m.  6 - m is a float: off by 2 at most upwards (where m's last bit is worth 4 or 8, from 2^25 on; beyond, it is
 // -m), so a weight is 2^14 at most, a half, whatever the scores.
 constexpr float kHeadroom = 6.f, kRise = 6.f; // (log2)
-// s is a product that the weight's fused multiply-add does not round, and the maximum does: beyond this they may differ by as much as a weight's
-// rounding and more (from 2^25 on weights would be no halves), so such rows' scores are rounded and taken less m first.
+// Where the scale is applied in the weight's fused multiply-add, s is a product that this does not round, and the maximum does: beyond this they may differ by a
+// sixteenth and more (from 2^25 on weights would be no halves), so such rows' scores are rounded and taken less m first.
 constexpr float kFar = 1048576.f;
 __device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && m != -FLT_MAX; }
 
@@ -47,7 +47,8 @@ struct PagedArgs {
     int min_share;      // rounds
     float scale2;       // |sm_scale| log2(e)
     unsigned q_sign;    // sign of sm_scale, in both halves
-    float cap_in, cap_out, cap_poly[3];   // softcap (cap_scores), cap_in 0: none
+    float cap_in, cap_out, cap_poly[3];   // softcap: cap_out - 2 cap_out / (2^(s cap_in) + 1), or cap_scores; cap_in 0: none
+    int mods;           // kPlain ...
 };
 
 __device__ __forceinline__ int token_of(const PagedArgs &a, int row) { return (int)(((unsigned long long)(unsigned)row * a.group_inverse) >> a.group_shift); }
@@ -368,11 +369,16 @@ __device__ __forceinline__ float attended_or_zero(float s, int keys, int bit) {
     return __uint_as_float(__float_as_uint(s) & (unsigned)((int)((unsigned)keys << (31 - bit)) >> 31));
 }
 
-// A lane's 16 scores q . k to cap tanh(s / cap), s the scaled ones, in units of log2: with x = 2 log2(e) s / cap that is cap - 2 cap / (2^x + 1),
-// a difference of numbers of the cap's size, so it serves where a score is no smaller than that, |x| > 1 for the lane's largest.  Otherwise
-// tanh(y) = y (1 + ...), a polynomial in x^2 (least maximum of the relative error on |x| <= 1, 2^-24.6) times the scale, whose error is relative to
-// the score: a cap far above the scores is none.  A lane has keys of one row, those that it does not attend are zero here, and lanes choose for
-// themselves: what a row gets follows from what it attends alone.  A mixed step of capped scores takes 97.6 us, 96.6 with the first form alone.
+// What a kernel does to scores: nothing, a cap of up to kLargeCap and a bias, or a larger cap and a bias.
+enum { kPlain, kModified, kLargelyCapped };
+// cap tanh(s / cap) is cap - 2 cap / (2^x + 1), x = 2 log2(e) s / cap: a difference of numbers of the cap's size, off by 14 2^-24 caps at most (the
+// roundings of x, 2^x, the sum, its reciprocal, the product and the difference).  Up to this cap that is 2^-12, half a weight's rounding, whatever the score.
+constexpr float kLargeCap = 256.f;
+// A lane's 16 scores q . k under a larger cap, in units of log2: the same where the lane's largest has |x| > 1, the cap being below three times that
+// score.  Otherwise tanh(y) = y (1 + ...), a polynomial in x^2 (least maximum of the relative error on |x| <= 1, 2^-24.6) times the scale, whose error is relative
+// to the score: a cap far above the scores is none.  A lane has keys of one row, those that it does not attend are zero here, and lanes choose for
+// themselves: what a row gets follows from what it attends alone.  A mixed step takes 96.2 us with the first form alone, 94.4 with the polynomial, and up to 111 with both
+// in a wavefront (a cap near three times the largest scores), so smaller caps have the first form only.
 constexpr float kCapPoly[3] = {-4.00369909e-02f, 1.91897040e-03f, -8.53218143e-05f};
 template <typename Get, typename Set>
 __device__ __forceinline__ void cap_scores(const PagedArgs &a, float scale2, Get get, Set set) {

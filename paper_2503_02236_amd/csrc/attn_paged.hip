@@ -42,7 +42,7 @@ using namespace paged;
 
 namespace {
 
-template <int D, int V, bool COPIES, bool MODS>
+template <int D, int V, bool COPIES, int MODS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_paged_kernel(PagedArgs a) {
     constexpr int P = D / V, ES = 2 * V;
     constexpr int CH = D / 32;                   // channels per lane of an operand V^T
@@ -227,14 +227,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                         }
                     }
                 }
-                if constexpr (MODS) {   // (two uniform branches: a choice per score would compute both sides)
-                    if (a.cap_in > 0.f) {
+                if constexpr (MODS) {   // (uniform branches: a choice per score would compute both sides)
+                    if constexpr (MODS == kLargelyCapped) {
                         if (!((t0 + 31 <= pos_f && t0 + 31 < pc.len && (a.window == 0 || pos_l - t0 < a.window)) || t0 + 32 <= pc.prefix)) {
                             const int see = attended_keys(t0 + 16 * lh, see_from, see_to, pc.prefix);
 #pragma unroll
                             for (int e = 0; e < 16; ++e) s[e] = attended_or_zero(s[e], see, 4 * (e & 3) + (e >> 2));
                         }
                         cap_scores(a, scale2, [&](int e) { return s[e]; }, [&](int e, float x) { s[e] = x; });
+                    } else if (a.cap_in > 0.f) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s[e] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e] * a.cap_in) + 1.f);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s[e] *= scale2;
@@ -510,19 +514,20 @@ PagedPlan paged_plan(const vq_kv_pages_t *kv, const vq_paged_batch_t *b) {
     return p;
 }
 
-template <int D, int V, bool COPIES, bool MODS>
+template <int D, int V, bool COPIES, int MODS>
 int run_wide(const PagedArgs &a, hipStream_t s) {
     static KernelSetup setup;
     if (int st = kernel_setup(reinterpret_cast<const void *>(&attn_paged_kernel<D, V, COPIES, MODS>), kLds, true, setup)) return st;
     attn_paged_kernel<D, V, COPIES, MODS><<<a.H * a.workers, kThreads, kLds, s>>>(a);
     return merge<D>(a, s);
 }
-template <int D, int V>
-int run_paged_as(const PagedArgs &a, hipStream_t s) {
-    const bool mods = a.cap_in > 0.f || a.slopes;
-    if (a.G == 1) return mods ? run_wide<D, V, true, true>(a, s) : run_wide<D, V, true, false>(a, s);
-    return mods ? run_wide<D, V, false, true>(a, s) : run_wide<D, V, false, false>(a, s);
+template <int D, int V, bool COPIES>
+int run_wide_with(const PagedArgs &a, hipStream_t s) {
+    if (a.mods == kPlain) return run_wide<D, V, COPIES, kPlain>(a, s);
+    return a.mods == kModified ? run_wide<D, V, COPIES, kModified>(a, s) : run_wide<D, V, COPIES, kLargelyCapped>(a, s);
 }
+template <int D, int V>
+int run_paged_as(const PagedArgs &a, hipStream_t s) { return a.G == 1 ? run_wide_with<D, V, true>(a, s) : run_wide_with<D, V, false>(a, s); }
 
 }  // namespace
 
@@ -578,6 +583,7 @@ int launch_attn_paged(const vq_kv_pages_t *kv, const vq_paged_batch_t *b, const 
     a.cap_in = b->softcap > 0.f ? std::min(2.f * a.scale2 / b->softcap, FLT_MAX) : 0.f;
     a.cap_out = std::min(b->softcap * kLog2e, FLT_MAX / 4);
     for (int i = 0; i < 3; ++i) a.cap_poly[i] = kCapPoly[i] * a.scale2;
+    a.mods = a.cap_in > 0.f && b->softcap > kLargeCap ? kLargelyCapped : a.cap_in > 0.f || b->slopes ? kModified : kPlain;
     if (p.few) return launch_few(a, kv->v, s);
     if (kv->D == 64) return kv->v == 8 ? run_paged_as<64, 8>(a, s) : kv->v == 4 ? run_paged_as<64, 4>(a, s) : run_paged_as<64, 2>(a, s);
     return kv->v == 8 ? run_paged_as<128, 8>(a, s) : kv->v == 4 ? run_paged_as<128, 4>(a, s) : run_paged_as<128, 2>(a, s);

@@ -18,7 +18,7 @@ using namespace paged;
 
 namespace {
 
-template <int V, bool COPIES, bool MODS>
+template <int V, bool COPIES, int MODS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_paged_few_kernel(PagedArgs a) {
     constexpr int D = 128, P = D / V, ES = 2 * V, ROWS = 16, KEYS = 64;
     constexpr int KW = P / 16;                   // dwords of a lane's K codes of a key: its 32 channels
@@ -170,13 +170,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             auto body = [&](int tile, Codes &codes, const Codes &after, const Codes &second) {
                 const int idx = idx0 + (tile << 3), t0 = (idx < pc.front ? idx : pc.lo + idx - pc.front) * KEYS;
                 if constexpr (MODS) {
-                    if (a.cap_in > 0.f) {
+                    if constexpr (MODS == kLargelyCapped) {
                         if (__builtin_expect((unsigned)(t0 - all_from) > all_span, 0)) {
                             const int see = attended_keys(t0 + 16 * g, see_from, see_to, pc.prefix);
 #pragma unroll
                             for (int e = 0; e < 16; ++e) s[e / 4][e % 4] = attended_or_zero(s[e / 4][e % 4], see, 4 * (e % 4) + e / 4);
                         }
                         cap_scores(a, scale2, [&](int e) { return s[e / 4][e % 4]; }, [&](int e, float x) { s[e / 4][e % 4] = x; });
+                    } else if (a.cap_in > 0.f) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s[e / 4][e % 4] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[e / 4][e % 4] * a.cap_in) + 1.f);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s[e / 4][e % 4] *= scale2;
@@ -363,19 +367,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
-template <int V, bool COPIES, bool MODS>
+template <int V, bool COPIES, int MODS>
 int run_few(const PagedArgs &a, hipStream_t s) {
     static KernelSetup setup;
     if (int st = kernel_setup(reinterpret_cast<const void *>(&attn_paged_few_kernel<V, COPIES, MODS>), kLds, true, setup)) return st;
     attn_paged_few_kernel<V, COPIES, MODS><<<a.H * a.workers, kThreads, kLds, s>>>(a);
     return merge<128>(a, s);
 }
-template <int V>
-int run_few_as(const PagedArgs &a, hipStream_t s) {
-    const bool mods = a.cap_in > 0.f || a.slopes;
-    if (a.G == 1) return mods ? run_few<V, true, true>(a, s) : run_few<V, true, false>(a, s);
-    return mods ? run_few<V, false, true>(a, s) : run_few<V, false, false>(a, s);
+template <int V, bool COPIES>
+int run_few_with(const PagedArgs &a, hipStream_t s) {
+    if (a.mods == kPlain) return run_few<V, COPIES, kPlain>(a, s);
+    return a.mods == kModified ? run_few<V, COPIES, kModified>(a, s) : run_few<V, COPIES, kLargelyCapped>(a, s);
 }
+template <int V>
+int run_few_as(const PagedArgs &a, hipStream_t s) { return a.G == 1 ? run_few_with<V, true>(a, s) : run_few_with<V, false>(a, s); }
 
 }  // namespace
 

@@ -7,10 +7,11 @@ U = 2.0 ** -24     # half a step of fp32, relative
 def attend(case):
     """(out, bound on the error of an fp32 computation with fp16 weights) [rows][Hq][D].
 
-    Bound, term by term: a score is a sum of D exact products in fp32 in some order, D + 2 roundings of sum |q k|, scaled.  A capped one:
-    where every |2 log2(e) s / cap| of a row is 1 or less, an odd polynomial of the score, 6 roundings of the result; elsewhere cap (1 - 2 / (2^x + 1)),
-    in units of cap U: its factors' rounding 2 + 2, 2^x 1, the sum 2, the reciprocal 4, product and difference 3 -- and then the cap is below 2.9 times the row's
-    largest score, so that the error never grows with the cap.  A biased score: 4 roundings of the bias.  2^x and the difference to the
+    Bound, term by term: a score is a sum of D exact products in fp32 in some order, D + 2 roundings of sum |q k|, scaled.  A capped one
+    is cap (1 - 2 / (2^x + 1)), in units of cap U: its factors' rounding 2 + 2, 2^x 1, the sum 2, the reciprocal 4, product and difference 3: 14, for a cap of 256
+    2^-12, half of what a weight's rounding allows.  Under a larger cap that form serves only where |x| = |2 log2(e) s / cap| passes 1 in a row, the cap then being
+    below 2.9 times the row's largest score, so that the error never grows with the cap; elsewhere an odd polynomial of the score, 6 roundings of the
+    result.  A biased score: 4 roundings of the bias.  2^x and the difference to the
     maximum: 4 of the score and of the largest.  A weight is rounded to a half (2^-11 of it, 2^-31 of the largest where it is a subnormal one; below
     that it may vanish); the output is (2^-11)."""
     Hq = case.H * case.group
@@ -34,7 +35,8 @@ def attend(case):
             if case.softcap:
                 top = np.where(see, np.abs(s), 0.0).max(1, keepdims=True)
                 s = case.softcap * np.tanh(s / case.softcap)
-                ds = ds + 14 * U * np.where(2.885 * top < 0.999 * case.softcap, 0.0, np.minimum(case.softcap, 2.9 * top)) + 6 * U * np.abs(s)
+                ds = ds + 6 * U * np.abs(s) + 14 * U * (case.softcap if case.softcap <= 256 else np.where(
+                    2.885 * top < 0.999 * case.softcap, 0.0, np.minimum(case.softcap, 2.9 * top)))
             if case.slopes is not None:
                 bias = float(case.slopes[hq]) * np.abs(pos - t)
                 s = s - bias

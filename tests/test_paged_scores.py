@@ -27,7 +27,7 @@ def test_the_capped_reference_is_the_cap_itself():
     b, bb = paged_reference.attend(free)
     assert np.abs(a - b).max() <= 1e-12 and (ba <= bb + 1e-5).all()
     f = np.float32
-    for cap in (1e-3, 3.0, 30.0, 1e4, 1e6, 3e38):
+    for cap in (1e-3, 3.0, 30.0, 256.0, 257.0, 1e4, 1e6, 3e38):
         s = rng.normal(0, 2, 4096).astype(np.float32)
         x = s * f(min(2 * 1.4426950408889634 / cap, np.finfo(np.float32).max))
         w = x * x
@@ -36,15 +36,15 @@ def test_the_capped_reference_is_the_cap_itself():
         small = s * (w * (w * (w * c[2] + c[1]) + c[0]) + scale) / scale
         with np.errstate(over="ignore"):
             large = f(cap) - f(2) * (f(cap) / (np.exp2(x) + f(1)))
-        got = np.where(np.abs(x).max() <= 1, small, large).astype(np.float64)
+        got = (small if cap > 256 and np.abs(x).max() <= 1 else large).astype(np.float64)
         want = cap * np.tanh(s.astype(np.float64) / cap)
         top = np.abs(s).max()
-        allowed = 6 * 2.0 ** -24 * np.abs(want) + (0 if 2.885 * top < 0.999 * cap else 14 * 2.0 ** -24 * min(cap, 2.9 * top))
+        allowed = 6 * 2.0 ** -24 * np.abs(want) + 14 * 2.0 ** -24 * (cap if cap <= 256 else 0 if 2.885 * top < 0.999 * cap else min(cap, 2.9 * top))
         assert (np.abs(got - want) <= allowed).all(), cap
 
 
 @gpu
-@pytest.mark.parametrize("softcap", [1e-42, 1e-30, 0.01, 3.0, 50.0, 1e4, 1e6, 1e8, 1.2e38, 3.0e38, float(np.finfo(np.float32).max)])
+@pytest.mark.parametrize("softcap", [1e-42, 1e-30, 0.01, 3.0, 50.0, 256.0, 257.0, 1e4, 1e6, 1e8, 1.2e38, 3.0e38, float(np.finfo(np.float32).max)])
 @pytest.mark.parametrize("kw", KERNELS)
 def test_a_cap_of_any_size(gpu_device, softcap, kw):
     """A large cap is none, a small one leaves equal scores; zero scores stay zero under both."""
@@ -63,7 +63,18 @@ def test_caps_with_masks_and_biases(gpu_device, softcap, kw, mods):
 
 
 @gpu
-@pytest.mark.parametrize("softcap", [2.0, 40.0])
+@pytest.mark.parametrize("softcap", [257.0, 600.0])
+@pytest.mark.parametrize("kw", KERNELS)
+@pytest.mark.parametrize("mods", [dict(), dict(window=20, prefix=[5, 0, 300, 40, 0, 1]), dict(slopes=[0.5, 0.01, 2.0, -0.02])])
+def test_scores_on_both_sides_of_a_large_cap(gpu_device, softcap, kw, mods):
+    """Scores of hundreds beside small ones: lanes of a wavefront take either form of the cap."""
+    case = make(REQS, seed=5, softcap=softcap, sigma=10.0, sm_scale=0.6, extra_rows=1, **kw, **mods)
+    case.q[1::3] *= np.float16(0.125)
+    paged_reference.check(case, attend(case, gpu_device))
+
+
+@gpu
+@pytest.mark.parametrize("softcap", [2.0, 40.0, 300.0, 1e5])
 @pytest.mark.parametrize("kw", KERNELS)
 def test_capped_rows_ignore_what_they_do_not_attend(gpu_device, softcap, kw):
     """Codes behind a request's end that name large or infinite entries: the very same bits."""
@@ -79,7 +90,7 @@ def test_capped_rows_ignore_what_they_do_not_attend(gpu_device, softcap, kw):
 # ------------------------------------------------------------------------------------------------ rows and their neighbours
 
 @gpu
-@pytest.mark.parametrize("mods", [dict(), dict(softcap=30.0), dict(slopes=[0.0, 0.01, 0.0, 0.02])])
+@pytest.mark.parametrize("mods", [dict(), dict(softcap=30.0), dict(softcap=300.0, sm_scale=3.0), dict(slopes=[0.0, 0.01, 0.0, 0.02])])
 @pytest.mark.parametrize("kw", KERNELS)
 def test_a_row_does_not_depend_on_its_neighbours_queries(gpu_device, kw, mods):
     """Every other row's query changes, to one whose scores grow from tile to tile and to ones of other sizes: the rest keep every bit."""
